@@ -380,7 +380,7 @@ def _plain_assign(state):
     block = tables[b, (pos // page).clamp(max=W - 1)].long()
     slots = torch.where(inside & ok[b], block * page + pos % page, -1)
     starts = torch.cat((torch.zeros_like(ends[:1]), ends))
-    taken = torch.where(ok, incl, 0).amax()
+    taken = torch.where(ok & (extra > 0), incl, 0).amax()
     counts = torch.stack(((count - taken)[0], ends[-1], (~ok).sum()))
     seq = torch.where(ok, ctx + new, 0)
     return slots.int(), pos.int(), seq.int(), starts.int(), counts.int(), tables
