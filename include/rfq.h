@@ -451,6 +451,183 @@ rfq_status rfq_hif4_gemm_split(const uint8_t *q_codes, const uint32_t *q_meta,
 int64_t rfq_hif4_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K);
 
 /*
+ * Attention over a key/value cache held in MXFP4.  The calls below take a
+ * decoder layer's q, k and v from its quantized projection to the input of
+ * its output projection: the step's tokens get blocks of the cache
+ * (rfq_block_assign), q and k are turned by their positions, k and v are
+ * quantized into the cache (rfq_kv_append), and the queries attend to it
+ * (rfq_kv_attention).  rfq_rope and rfq_rope_backward are the rotation by itself,
+ * for training and for models without a cache.
+ */
+
+/* Tokens x heads x D elements: element (t, h, d) is at
+ * data[t * token_stride + h * head_stride + d] (strides in elements, >= 0 for
+ * inputs, > 0 for outputs of more than one token or head).  data is 16-byte
+ * aligned and both strides are multiples of 16 bytes (RFQ_ERR_ALIGN).  The
+ * struct is in host memory and read during the call. */
+typedef struct rfq_heads {
+    void *data;
+    int64_t token_stride;
+    int64_t head_stride;
+} rfq_heads;
+
+/* Rotary positions with several axes (host memory, read during the call).  The
+ * first `rotary` channels of a head form rotary / 2 pairs: (j, j + rotary / 2),
+ * or with interleaved nonzero (2 j, 2 j + 1).  Pair j of token t is turned by the
+ * angle whose cosine and sine are cos_sin[p][j], with p = positions[axes[j]][t]:
+ *     (a, b) -> (a c - b s, b c + a s),
+ * each product and sum rounded to fp32.  Channels from `rotary` on are copied.
+ *   positions  device [n_axes][T], axis a at positions + a * positions_stride
+ *              (elements).  A position outside [0, max_pos) gives NaN.
+ *   cos_sin    device [max_pos][rotary / 2][2] fp32, 8-byte aligned.
+ *   axes       host [rotary / 2], each below n_axes; NULL: axis 0 for every pair.
+ *   n_axes     1 .. 8;  rotary: a multiple of 16, 16 .. D. */
+typedef struct rfq_rope_spec {
+    const int32_t *positions;
+    int64_t positions_stride;
+    const float *cos_sin;
+    int64_t max_pos;
+    const uint8_t *axes;
+    int32_t n_axes;
+    int32_t rotary;
+    int32_t interleaved;
+} rfq_rope_spec;
+
+/* A cache of `blocks` blocks of `page` tokens for `heads` key/value heads of D
+ * channels: codes [blocks][heads][page][D / 2] and E8M0 scales
+ * [blocks][heads][page][D / 32] of keys and of values, MXFP4 as above (blocks of
+ * 32 channels).  Slot s is token s % page of block s / page.  All four pointers
+ * are 16-byte aligned; the struct is in host memory and read during the call.
+ *   page: 16, 32, 64, 128 or 256;  D: 64, 128 or 256;  blocks * page < 2^31. */
+typedef struct rfq_kv_cache {
+    uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+    int64_t blocks, heads, page, D;
+} rfq_kv_cache;
+
+/*
+ * Blocks, slots and positions of one step's tokens, from the requests' lengths
+ * on the device.  Request b holds ctx_lens[b] tokens in the blocks
+ * block_tables[b][0 .. ceil(ctx / page) - 1] and adds new_lens[b] tokens (negative
+ * lengths count as 0).  The blocks that it lacks are taken from the end of the
+ * list of free ones, request by request: the n-th block taken in the step is
+ * free_blocks[count - 1 - n], count being free_count[0] (cut to [0, n_free]).
+ * A request is refused, and gets no block, where its tokens do not fit the
+ * table's width, or where it lacks blocks and the list holds fewer than it and the
+ * requests before it that fit the width lack together (refused ones included: once
+ * the list is short, every later request that lacks blocks is refused).
+ *   block_tables  [B][width], written where blocks were taken (and only there).
+ *   slots         [tokens]: the slot of each new token in the order of requests, -1
+ *                 for tokens of refused requests and past the last token.
+ *   positions     [tokens]: the token's place in its request (0 past the last).
+ *   seq_lens      [B]: ctx + new, or 0 for a refused request.
+ *   query_starts  [B + 1]: the requests' first rows among the new tokens.
+ *   counts        [3]: free blocks left, new tokens, refused requests.  counts may
+ *                 not overlap free_count; its first element is the free_count of
+ *                 the next call.
+ * tokens may exceed the number of new tokens (a captured step of fixed size); where
+ * it is smaller, the tokens past it get neither slot nor block.  page: as
+ * rfq_kv_cache.  B at most 16384; B == 0 writes slots, positions, query_starts[0]
+ * and counts.  Calling it again with the same inputs writes the same values.
+ */
+rfq_status rfq_block_assign(const int32_t *ctx_lens, const int32_t *new_lens, int64_t B,
+                            int32_t *block_tables, int64_t width, const int32_t *free_blocks,
+                            int64_t n_free, const int32_t *free_count, int64_t page,
+                            int64_t tokens, int32_t *slots, int32_t *positions,
+                            int32_t *seq_lens, int32_t *query_starts, int32_t *counts,
+                            void *hip_stream);
+
+/*
+ * Gives the blocks of ended requests back: the first ceil(lens[b] / page) entries
+ * (at most width) of block_tables[b], for each b with ended[b] != 0 and in their
+ * order, are written to free_blocks from free_count[0] (cut to [0, n_free]) on;
+ * what does not fit the list is dropped.  free_count_out [1] receives the new count
+ * and may not overlap free_count.  B at most 16384.
+ */
+rfq_status rfq_block_release(const int32_t *lens, const uint8_t *ended, int64_t B,
+                             const int32_t *block_tables, int64_t width, int32_t *free_blocks,
+                             int64_t n_free, const int32_t *free_count, int64_t page,
+                             int32_t *free_count_out, void *hip_stream);
+
+/*
+ * y = x with its heads rotated (rfq_rope_spec), fp32 arithmetic, rounded once to
+ * dtype.  x and y are [T][H][D] of the same dtype; they may be the same tensor (with
+ * the same strides) and may not overlap otherwise.
+ *   D a multiple of 16, at most 512;  T, H below 2^31 (T < 2^31 / 16).
+ */
+rfq_status rfq_rope(const rfq_heads *x, rfq_dtype dtype, int64_t T, int64_t H, int64_t D,
+                    const rfq_rope_spec *rope, const rfq_heads *y, void *hip_stream);
+
+/* The gradient of rfq_rope: dx from dy, the rotation by the opposite angle. */
+rfq_status rfq_rope_backward(const rfq_heads *dy, rfq_dtype dtype, int64_t T, int64_t H,
+                             int64_t D, const rfq_rope_spec *rope, const rfq_heads *dx,
+                             void *hip_stream);
+
+/*
+ * Writes T tokens into a cache: k (rotated where rope is given) and v are quantized
+ * to MXFP4 and stored in slots[t].  The codes are those of rfq_quantize_act on the
+ * rotated fp32 values, which are not rounded in between.  A block that holds an
+ * infinity or a NaN gets the scale byte 0xFF (NaN) and zero codes.  Tokens whose
+ * slot is outside the cache (negative: padding) are not stored; of two tokens with
+ * the same slot either may be the one kept.  With q given, q_out receives q rotated,
+ * as rfq_rope, for every token.
+ *   k, v   [T][cache->heads][D] of dtype;  q, q_out [T][Hq][D] of dtype, or both
+ *          NULL; rope may be NULL only without q.  q_out may be q itself.
+ *   slots  [T] int32.
+ */
+rfq_status rfq_kv_append(const rfq_heads *k, const rfq_heads *v, rfq_dtype dtype, int64_t T,
+                         const int32_t *slots, const rfq_kv_cache *cache,
+                         const rfq_heads *q, int64_t Hq, const rfq_rope_spec *rope,
+                         const rfq_heads *q_out, void *hip_stream);
+
+/*
+ * Reads slots back: k_out and v_out [n][cache->heads][D] dense, fp32 or bf16 (both
+ * hold every MXFP4 value of rfq_kv_append exactly); 16-byte aligned.  A slot outside
+ * the cache gives zeros, the scale byte 0xFF NaN.
+ */
+rfq_status rfq_kv_gather(const rfq_kv_cache *cache, const int32_t *slots, int64_t n,
+                         void *k_out, void *v_out, rfq_dtype out_dtype, void *hip_stream);
+
+/*
+ * Attention of the queries of B requests over their cached keys and values.
+ * Request b holds the tokens 0 .. len - 1 (len = seq_lens[b], cut to [0, width *
+ * page]), token j in block block_tables[b][j / page]; its queries are the rows
+ * query_starts[b] .. query_starts[b + 1] - 1 of q, the last of them at token len - 1,
+ * so row i of nq is at p = len - nq + i.  Row i attends to the tokens j with j < len,
+ * with j <= p if causal is nonzero, and with j > p - window if window > 0:
+ *     out = sum_j P_j v_j / sum_j P_j,  P_j = exp(scale q . k_j),
+ *     lse = log sum_j P_j.
+ * Query head h reads key/value head h / (Hq / cache->heads).  A row that attends to
+ * no token gives zeros, and lse -infinity.  Tokens whose table entry is outside
+ * [0, blocks) are not attended to.  What stands in masked or unused places of the
+ * cache has no influence.  A NaN key block or value block (scale byte 0xFF, for
+ * values from 0xFD, which bf16 does not hold) makes NaN of every row that attends to
+ * its token.  Rows of q that belong to no request are not written.
+ * q . k is summed in fp32 from exact products; the sums of P and of P v are fp32,
+ * with P rounded to bf16 (relative 2^-9) as a matrix-core operand of the latter.
+ *   q, out   [T][Hq][D] bf16;  Hq a multiple of cache->heads.
+ *   lse      [T][Hq] fp32 or NULL.
+ *   block_tables [B][width];  seq_lens [B];  query_starts [B + 1], not decreasing.
+ *   max_query, max_seq: the largest number of queries and of tokens of a request,
+ *            by which the work is divided; a value that is too small costs time
+ *            only.
+ *   workspace: device memory, 16-byte aligned, not read before it is written; with
+ *            fewer than rfq_kv_attention_workspace_bytes bytes (or NULL, 0) a
+ *            request's tokens are not split over workgroups.
+ * Calls that share a workspace must be ordered.  T, B, Hq below 2^24, T * Hq < 2^31.
+ */
+rfq_status rfq_kv_attention(const rfq_heads *q, int64_t T, int64_t Hq, const rfq_kv_cache *cache,
+                            const int32_t *block_tables, int64_t width,
+                            const int32_t *seq_lens, const int32_t *query_starts, int64_t B,
+                            int64_t max_query, int64_t max_seq, float scale, int causal,
+                            int64_t window, const rfq_heads *out, float *lse,
+                            void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/* Workspace of rfq_kv_attention for these arguments (0 where it splits nothing, or
+ * for sizes it rejects).  Host-only. */
+int64_t rfq_kv_attention_workspace_bytes(int64_t T, int64_t Hq, int64_t heads, int64_t D,
+                                         int64_t B, int64_t max_query, int64_t max_seq);
+
+/*
  * Measurement support, not a step of the method: the sustained rate of the
  * FP4 matrix cores that the product (Eq. 11) runs on, without memory
  * traffic.  256 workgroups of 8 waves (one per CU of the MI355X, two waves

@@ -12,3 +12,8 @@ from .rfq import (  # noqa: F401
     rfq_gemm_split, rfq_gemm_split_noalloc, rfq_gemm_workspace_bytes, rfq_mfma_bf16_loop, rfq_mfma_fp4_loop,
     rfq_swiglu_quantize_act,
 )
+from .kv import (  # noqa: F401
+    KvCache, kv_cache, rfq_block_assign, rfq_block_release, rfq_kv_append, rfq_kv_attention,
+    rfq_kv_attention_workspace_bytes, rfq_kv_gather, rfq_rope, rfq_rope_backward, rope_axes,
+    rope_table,
+)

@@ -9,6 +9,7 @@
 
 #include <atomic>
 
+#include "kv.h"
 #include "rfq.h"
 #include "rfq_internal.h"
 
@@ -81,7 +82,11 @@ bool hif4_product_fits(int64_t M, int64_t N) {
          rows * ((N + 127) / 128) * 640 <= kMaxWorkItems;
 }
 
-// Confirms that the current device is a gfx950 GPU (cached per device).
+rfq_status launched(hipError_t e) { return e == hipSuccess ? RFQ_OK : RFQ_ERR_LAUNCH; }
+
+}  // namespace
+
+namespace rfq {
 rfq_status check_device() {
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0) return RFQ_ERR_DEVICE;
@@ -95,10 +100,11 @@ rfq_status check_device() {
   }
   return st == 1 ? RFQ_OK : RFQ_ERR_DEVICE;
 }
+}  // namespace rfq
 
-rfq_status launched(hipError_t e) { return e == hipSuccess ? RFQ_OK : RFQ_ERR_LAUNCH; }
-
-}  // namespace
+namespace {
+using rfq::check_device;
+}
 
 extern "C" {
 

@@ -1,0 +1,575 @@
+// Attention of a step's queries over an MXFP4 key/value cache (block tables).
+//
+// For a key/value head, the rows are its group's query heads times the request's
+// queries (row r: query r / group, head r % group).  With the keys' tile as the left
+// operand the scores come out transposed, S^T = K Q^T: a lane holds one row's
+// scores of 16 tokens (4 of each 16-token piece), which is the layout in which
+// O^T = V^T P^T takes P as its right operand, so P goes from one product to the
+// next in the lane's own registers.  The running maximum m, sum l and accumulator O
+// of a row follow each tile of 64 tokens: with m' = max(m, max S), O and l are scaled
+// by exp(m - m') and exp(S - m') V is added; exponentials are base 2 with log2(e)
+// folded into the scale.
+//
+// Codes are decoded to bf16 in registers (exact: two significant bits and a
+// power-of-two scale) and multiplied by the bf16 matrix cores with fp32 sums.  The
+// FP4 matrix instructions could take the keys' codes as they are against q split in
+// two FP8 terms, but their sums keep about 2^-18 of the terms' sum (measured on
+// 16 x 16 x 128; bf16: 2^-25), which shows in lse.  A lane loads a quarter of a token's
+// channels, one 16-byte load at 128 channels, with one scale byte; keys go straight to
+// the operand, values through LDS rows of bf16, from which the transposing read
+// takes them token by token.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "kv.h"
+#include "mx_device.h"
+#include "rfq_internal.h"
+
+namespace rfq {
+namespace {
+
+constexpr int kThreads = 256, kWaves = 4;
+// Workgroups that the split kernel's work is divided over: two per CU.
+constexpr int kSplitGroups = 512;
+constexpr float kLn2 = 0.69314718055994531f;
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Maximum / sum over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
+__device__ __forceinline__ float across_max(float v) {
+  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float across_sum(float v) {
+  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+__device__ __forceinline__ uint32_t c_byte(uint32_t w, int i) { return w >> (8 * i) & 0xFFu; }
+
+// 8 codes to bf16 times their block's scale.
+__device__ __forceinline__ u32x4 decode_bf16(uint32_t c, float s) {
+  u32x4 r;
+  r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0));
+  r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1));
+  r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2));
+  r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3));
+  return r;
+}
+
+__device__ __forceinline__ v4f mma(const u32x4 &a, const u32x4 &b, const v4f &c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                 __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// Element i of lane l: 16-bit element (l mod 16) of row 4 (l / 16) + i, each lane
+// pointing at 4 elements: lanes 4 j .. 4 j + 3 of a group of 16 at its row j.
+__device__ __forceinline__ u32x2 read_transposed(const uint8_t *p) {
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p));
+}
+
+// ---- the shapes and the requests
+
+template <int D, int NT>
+struct Shape {
+  static constexpr int kRows = 16 * NT;
+  // Tokens of a wave's step, in pieces of 16: the codes of two steps are in
+  // registers (at 64 tokens of 256 channels they would be spilled).
+  static constexpr int kPieces = D == 256 ? 2 : 4;
+  static constexpr int kTile = 16 * kPieces;
+  static constexpr int kWords = D / 32;                  // code dwords of a lane and token
+  static constexpr int kPitch = 2 * D + 32;              // bytes of a value row in LDS
+  static constexpr int kCols = D / 16;                   // 16-channel tiles of O
+  static constexpr int kWaveLds = 32 * kPitch;           // >= 16 * D * 4
+};
+
+struct Request {
+  int start, nq, len;
+  int tiles0, tiles;                      // first token tile that a row sees; number (>= 1)
+  int row_tiles;
+};
+
+template <class S>
+__device__ __forceinline__ Request request(const AttentionArgs &a, int b) {
+  Request r;
+  const int s0 = min(max(a.starts[b], 0), a.T), s1 = min(max(a.starts[b + 1], s0), a.T);
+  r.start = s0;
+  r.nq = s1 - s0;
+  r.len = min(max(a.lens[b], 0), a.capacity);
+  int first = 0;
+  if (a.window) first = max(0, r.len - r.nq - a.window + 1);
+  r.tiles0 = min(first, r.len) / S::kTile;
+  r.tiles = max(1, (r.len + S::kTile - 1) / S::kTile - r.tiles0);
+  r.row_tiles = (r.nq * a.group + S::kRows - 1) / S::kRows;
+  return r;
+}
+// Units of work of a request: token tiles, or with whole items one per (head, row tile).
+__device__ __forceinline__ int64_t units(const AttentionArgs &a, const Request &r, bool split) {
+  return (int64_t)a.heads * r.row_tiles * (split ? r.tiles : 1);
+}
+
+// One part of a (request, head, row tile): where its partial result goes.
+struct Partial {
+  float *o;                               // [groups * 2][ROWS][D]
+  float *ml;                              // [groups * 2][ROWS][2]
+  int4 *item;                             // [groups] item whose first part ends the range
+};
+
+// A lane's codes and scale bytes of a tile of P pieces: token 16 u + lane % 16, channels
+// (lane / 16) D / 4 on.
+template <int D, int P>
+struct Codes {
+  using Vec = std::conditional_t<D == 64, u32x2, u32x4>;
+  static constexpr int kVecs = D == 256 ? 2 : 1;
+  Vec k[P][kVecs], v[P][kVecs];
+  uint32_t ks[P], vs[P];                  // D = 256: two bytes
+};
+
+template <int D, int NT>
+__global__ __launch_bounds__(kThreads, 2) void kv_attention_kernel(const AttentionArgs a,
+                                                                   const Partial part,
+                                                                   int split) {
+  using S = Shape<D, NT>;
+  constexpr int W = S::kWords, P = S::kPieces;
+  using Tile = Codes<D, P>;
+  __shared__ alignas(16) uint8_t lds_v[kWaves][S::kWaveLds];
+  __shared__ float lds_ml[kWaves][S::kRows][2];
+  __shared__ int64_t scan[kWaves];
+  __shared__ int64_t found_at;
+  __shared__ int found_b;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 15, g = lane >> 4;
+  const int wg = blockIdx.x, groups = gridDim.x;
+
+  // This workgroup's range [u0, u1) of the units of all requests.
+  int64_t total = 0, u0, u1, share;
+  {
+    const int per = (a.B + kThreads - 1) / kThreads;
+    const int b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
+    int64_t n = 0;
+    for (int b = b0; b < b1; ++b) n += units(a, request<S>(a, b), split);
+    int64_t incl = n;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int64_t o = __shfl_up(incl, d);
+      if (lane >= d) incl += o;
+    }
+    if (lane == 63) scan[wave] = incl;
+    __syncthreads();
+    int64_t before = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < wave) before += scan[w];
+      total += scan[w];
+    }
+    before += incl - n;
+    share = (total + groups - 1) / groups;
+    if (split && share < kWaves) share = kWaves;
+    u0 = share * wg;
+    u1 = u0 + share < total ? u0 + share : total;
+    if (u0 < u1 && before <= u0 && u0 < before + n) {
+      int b = b0;
+      for (;; ++b) {
+        const int64_t k = units(a, request<S>(a, b), split);
+        if (u0 < before + k) break;
+        before += k;
+      }
+      found_b = b;
+      found_at = before;
+    }
+    __syncthreads();
+  }
+  if (part.item && tid == 0) part.item[wg] = make_int4(0, 0, 0, 0);
+  if (u0 >= u1) return;
+  int b = __builtin_amdgcn_readfirstlane(found_b);
+  int64_t base = found_at;                // first unit of request b
+  Request req = request<S>(a, b);
+
+  uint8_t *vbuf = lds_v[wave];
+  const int lane_bytes = g * (D / 8);     // a lane's codes within a token's
+  const int scale_at = g * (D / 4) / 32;
+
+  for (int64_t u = u0; u < u1;) {
+    int64_t n = units(a, req, split);
+    while (u >= base + n) {               // next request that has work
+      base += n;
+      req = request<S>(a, ++b);
+      n = units(a, req, split);
+    }
+    const int nk = split ? req.tiles : 1;
+    const int64_t local = u - base;
+    const int item = (int)(local / nk), k0 = (int)(local - (int64_t)item * nk);
+    const int head = item / req.row_tiles, rt = item - head * req.row_tiles;
+    const int64_t left = u1 - u;
+    const int k1 = (int)(left < nk - k0 ? k0 + left : nk);
+    const int tile0 = req.tiles0 + (split ? k0 : 0);
+    const int tile1 = req.tiles0 + (split ? k1 : req.tiles);
+    u += k1 - k0;
+
+    // The lane's rows: one of each 16-row tile.
+    const int rows = req.nq * a.group, row0 = rt * S::kRows;
+    int lo[NT], hi[NT];
+    u32x4 qf[NT][W];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int r = row0 + 16 * t + col, i = r / a.group, h = r - i * a.group;
+      const int p = req.len - req.nq + i;
+      hi[t] = a.causal ? min(p, req.len - 1) : req.len - 1;
+      lo[t] = a.window ? p - a.window + 1 : 0;
+#pragma unroll
+      for (int w = 0; w < W; ++w) qf[t][w] = u32x4{0, 0, 0, 0};
+      if (r < rows) {
+        const uint16_t *q = a.q + (req.start + i) * a.q_ts +
+                            (head * a.group + h) * a.q_hs + g * (D / 4);
+#pragma unroll
+        for (int w = 0; w < W; ++w) qf[t][w] = *reinterpret_cast<const u32x4 *>(q + 8 * w);
+      }
+    }
+    // Tokens that every row sees: from all_lo to all_hi; none beyond [any_lo, any_hi].
+    const int last_row = min(row0 + S::kRows, rows) - 1;
+    const int i0 = row0 / a.group, i1 = last_row / a.group;
+    const int p0 = req.len - req.nq + i0, p1 = req.len - req.nq + i1;
+    const int all_hi = a.causal ? p0 : req.len - 1, any_hi = a.causal ? p1 : req.len - 1;
+    const int all_lo = a.window ? p1 - a.window + 1 : 0, any_lo = a.window ? p0 - a.window + 1 : 0;
+
+    v4f o[NT][S::kCols];
+    float m[NT], l[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      m[t] = neg_inf();
+      l[t] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < S::kCols; ++c) o[t][c] = v4f{0, 0, 0, 0};
+    }
+
+    const int32_t *table = a.tables + (int64_t)b * a.width;
+    // The codes of a tile, and which of its 16-token pieces have a block.
+    auto fetch = [&](int tile, Tile &c) -> uint32_t {
+      uint32_t have = 0;
+#pragma unroll
+      for (int s = 0; s < P; ++s) {
+        const int t0 = tile * S::kTile + 16 * s;
+        int id = -1;
+        if (t0 < req.len) id = table[t0 >> a.page_shift];
+        const bool ok = (uint32_t)id < (uint32_t)a.blocks;
+        have |= (uint32_t)ok << s;
+        if (!ok) id = 0;
+        const int64_t row =
+            ((((int64_t)id * a.heads + head) << a.page_shift) + (t0 & (a.page - 1))) + col;
+        const uint8_t *kc = a.k_codes + row * (D / 2) + lane_bytes;
+        const uint8_t *vc = a.v_codes + row * (D / 2) + lane_bytes;
+        const uint8_t *ks = a.k_scales + row * (D / 32) + scale_at;
+        const uint8_t *vs = a.v_scales + row * (D / 32) + scale_at;
+        using Vec = typename Tile::Vec;
+#pragma unroll
+        for (int i = 0; i < Tile::kVecs; ++i) {
+          c.k[s][i] = reinterpret_cast<const Vec *>(kc)[i];
+          c.v[s][i] = reinterpret_cast<const Vec *>(vc)[i];
+        }
+        if constexpr (W == 8) {
+          c.ks[s] = *reinterpret_cast<const uint16_t *>(ks);
+          c.vs[s] = *reinterpret_cast<const uint16_t *>(vs);
+        } else {
+          c.ks[s] = *ks;
+          c.vs[s] = *vs;
+        }
+      }
+      return have;
+    };
+
+    // The wave's tiles: every fourth of the range that some row sees.
+    int tile = tile0 + wave;
+    while (tile < tile1 && (tile + 1) * S::kTile <= any_lo) tile += kWaves;
+    const int end = min(tile1, (any_hi + S::kTile) / S::kTile);
+    Tile cur, nxt;
+    uint32_t have = 0, have_nxt = 0;
+    if (tile < end) have = fetch(tile, cur);
+    for (; tile < end; tile += kWaves) {
+      if (tile + kWaves < end) have_nxt = fetch(tile + kWaves, nxt);
+      const int t0 = tile * S::kTile;
+      const bool whole = have == (1u << P) - 1 && t0 >= all_lo && t0 + S::kTile - 1 <= all_hi &&
+                         t0 + S::kTile <= req.len;
+      // Scores.
+      v4f s[NT][P];
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) s[t][p] = v4f{0, 0, 0, 0};
+        // A block that is NaN: the keys' own byte 0xFF, or a value byte that bf16 does
+        // not hold; its token's scores become NaN.
+        bool nan = c_byte(cur.ks[p], 0) == 0xFFu || c_byte(cur.vs[p], 0) >= 0xFDu;
+        if constexpr (W == 8)
+          nan = nan || c_byte(cur.ks[p], 1) == 0xFFu || c_byte(cur.vs[p], 1) >= 0xFDu;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+          const float sc = scale_operand(c_byte(cur.ks[p], w / 4));
+          u32x4 kf = decode_bf16(cur.k[p][w / 4][w % 4], sc);
+          if (w == 0 && nan) kf[0] = 0x7FC07FC0u;
+#pragma unroll
+          for (int t = 0; t < NT; ++t) s[t][p] = mma(kf, qf[t][w], s[t][p]);
+        }
+      }
+      // Softmax statistics.
+      u32x2 pf[NT][P];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        float top = neg_inf();
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float x = s[t][p][i] * a.scale_log2;
+            if (!whole) {
+              const int tok = t0 + 16 * p + 4 * g + i;
+              const bool see = tok >= lo[t] && tok <= hi[t] && (have >> p & 1);
+              x = see ? x : neg_inf();
+            }
+            s[t][p][i] = x;
+            top = fmaxf(top, x);
+          }
+        }
+        top = fmaxf(across_max(top), m[t]);
+        const float ref = top == neg_inf() ? 0.0f : top;
+        if (__any(top > m[t])) {
+          const float f = exp2_hw(m[t] - ref);
+          l[t] *= f;
+#pragma unroll
+          for (int c = 0; c < S::kCols; ++c) o[t][c] *= f;
+        }
+        m[t] = top;
+        float sum = 0.0f;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          float e[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            e[i] = exp2_hw(s[t][p][i] - ref);
+            sum += e[i];
+          }
+          const bf16x4 r = {(__bf16)e[0], (__bf16)e[1], (__bf16)e[2], (__bf16)e[3]};
+          pf[t][p] = __builtin_bit_cast(u32x2, r);
+        }
+        l[t] += sum;
+      }
+      // Values, 32 tokens at a time.
+#pragma unroll
+      for (int half = 0; half < P / 2; ++half) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const int p = 2 * half + q;
+          uint8_t *row = vbuf + (16 * q + col) * S::kPitch + g * (D / 2);
+#pragma unroll
+          for (int w = 0; w < W; ++w) {
+            // Always finite: a masked token's P is 0 and has to give 0.
+            const uint32_t byte = c_byte(cur.vs[p], w / 4);
+            *reinterpret_cast<u32x4 *>(row + 16 * w) = decode_bf16(
+                cur.v[p][w / 4][w % 4], scale_operand(byte < 0xFDu ? byte : 0u));
+          }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        const uint8_t *src = vbuf + (4 * g + (col >> 2)) * S::kPitch + (col & 3) * 8;
+#pragma unroll
+        for (int c = 0; c < S::kCols; ++c) {
+          const u32x2 v0 = read_transposed(src + 32 * c);
+          const u32x2 v1 = read_transposed(src + 16 * S::kPitch + 32 * c);
+          const u32x4 vf = {v0[0], v0[1], v1[0], v1[1]};
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            const u32x4 pp = {pf[t][2 * half][0], pf[t][2 * half][1], pf[t][2 * half + 1][0],
+                              pf[t][2 * half + 1][1]};
+            o[t][c] = mma(vf, pp, o[t][c]);
+          }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+      }
+      cur = nxt;
+      have = have_nxt;
+    }
+
+    // The four waves' results joined, a 16-row tile at a time: each scales its O by
+    // exp2(m - M) and leaves it in its LDS rows; every thread adds four of them.
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      l[t] = across_sum(l[t]);
+      if (g == 0) {
+        lds_ml[wave][16 * t + col][0] = m[t];
+        lds_ml[wave][16 * t + col][1] = l[t];
+      }
+    }
+    __syncthreads();
+    const bool complete = !split || (k0 == 0 && k1 == nk);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      float top = neg_inf();
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, lds_ml[w][16 * t + col][0]);
+      const float ref = top == neg_inf() ? 0.0f : top;
+      float sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w)
+        sum += lds_ml[w][16 * t + col][1] * exp2_hw(lds_ml[w][16 * t + col][0] - ref);
+      const float f = exp2_hw(m[t] - ref);
+#pragma unroll
+      for (int c = 0; c < S::kCols; ++c)
+        *reinterpret_cast<v4f *>(vbuf + (c * 64 + lane) * 16) = o[t][c] * f;
+      __syncthreads();
+      const int r = row0 + 16 * t + col;
+      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+      const int slot = 2 * wg + (k0 > 0 ? 0 : 1);
+      const int i = r / a.group, h = head * a.group + (r - i * a.group);
+#pragma unroll
+      for (int c = wave; c < S::kCols; c += kWaves) {
+        v4f x = *reinterpret_cast<const v4f *>(lds_v[0] + (c * 64 + lane) * 16);
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w)
+          x += *reinterpret_cast<const v4f *>(lds_v[w] + (c * 64 + lane) * 16);
+        if (complete) {
+          if (r < rows) {
+            x *= inv;
+            const bf16x4 y = {(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+            *reinterpret_cast<u32x2 *>(a.out + (req.start + i) * a.o_ts + h * a.o_hs + 16 * c +
+                                       4 * g) = __builtin_bit_cast(u32x2, y);
+          }
+        } else {
+          *reinterpret_cast<v4f *>(part.o + ((int64_t)slot * S::kRows + 16 * t + col) * D +
+                                   16 * c + 4 * g) = x;
+        }
+      }
+      if (wave == 0 && g == 0) {
+        if (complete) {
+          if (a.lse && r < rows)
+            a.lse[(int64_t)(req.start + i) * a.Hq + h] =
+                sum == 0.0f ? neg_inf() : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+        } else {
+          float *ml = part.ml + ((int64_t)slot * S::kRows + 16 * t + col) * 2;
+          ml[0] = top;
+          ml[1] = sum;
+        }
+      }
+      __syncthreads();
+    }
+    if (!complete && k0 == 0 && tid == 0) {
+      // Its other parts are the first of the following workgroups' ranges.
+      const int parts = 1 + (int)((nk - k1 + share - 1) / share);
+      part.item[wg] = make_int4(b, head, rt, parts);
+    }
+  }
+}
+
+// The parts of the items that the split kernel began but did not finish in one
+// workgroup: part 0 in slot 2 w + 1, the following ones in slots 2 (w + i).  Added in
+// that order.
+template <int D, int NT>
+__global__ __launch_bounds__(kThreads) void kv_attention_join_kernel(const AttentionArgs a,
+                                                                     const Partial part) {
+  using S = Shape<D, NT>;
+  const int wg = blockIdx.x;
+  const int4 it = part.item[wg];
+  if (it.w == 0) return;
+  const Request req = request<S>(a, it.x);
+  constexpr int kLanes = D / 4;                          // threads of a row
+  const int row = blockIdx.y * (kThreads / kLanes) + threadIdx.x / kLanes;
+  const int r = it.z * S::kRows + row;
+  if (r >= req.nq * a.group) return;
+  const int c = threadIdx.x % kLanes * 4;
+  auto slot = [&](int i) { return (int64_t)(i == 0 ? 2 * wg + 1 : 2 * (wg + i)); };
+  float top = neg_inf();
+  for (int i = 0; i < it.w; ++i) top = fmaxf(top, part.ml[(slot(i) * S::kRows + row) * 2]);
+  const float ref = top == neg_inf() ? 0.0f : top;
+  float sum = 0.0f;
+  v4f x = {0, 0, 0, 0};
+  for (int i = 0; i < it.w; ++i) {
+    const float *ml = part.ml + (slot(i) * S::kRows + row) * 2;
+    const float f = exp2_hw(ml[0] - ref);
+    sum += ml[1] * f;
+    x += *reinterpret_cast<const v4f *>(part.o + (slot(i) * S::kRows + row) * D + c) * f;
+  }
+  x *= sum == 0.0f ? 0.0f : 1.0f / sum;
+  const int i = r / a.group, h = it.y * a.group + (r - i * a.group);
+  const bf16x4 y = {(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+  *reinterpret_cast<u32x2 *>(a.out + (req.start + i) * a.o_ts + h * a.o_hs + c) =
+      __builtin_bit_cast(u32x2, y);
+  if (a.lse && c == 0)
+    a.lse[(int64_t)(req.start + i) * a.Hq + h] =
+        sum == 0.0f ? neg_inf() : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Rows of a tile: 32 where a request's rows fill them and the registers allow.
+int row_fragments(int64_t rows, int64_t D) { return D < 256 && rows > 16 ? 2 : 1; }
+
+int64_t partial_bytes(int64_t D, int nt) {
+  return (int64_t)kSplitGroups * (2 * 16 * nt * (D + 2) * 4 + 16);
+}
+
+template <int D, int NT>
+hipError_t launch(const AttentionArgs &a, bool split, float *work, hipStream_t stream) {
+  using S = Shape<D, NT>;
+  Partial p = {};
+  unsigned grid;
+  if (split) {
+    p.o = work;
+    p.ml = work + (int64_t)kSplitGroups * 2 * S::kRows * D;
+    p.item = reinterpret_cast<int4 *>(p.ml + (int64_t)kSplitGroups * 2 * S::kRows * 2);
+    grid = kSplitGroups;
+  } else {
+    // At least as many workgroups as there are items, within a launch's limits.
+    const int64_t items = (up((int64_t)a.T * a.group, S::kRows) + a.B) * a.heads;
+    grid = (unsigned)(items < (1 << 20) ? items : (1 << 20));
+  }
+  kv_attention_kernel<D, NT><<<grid, kThreads, 0, stream>>>(a, p, split);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !split) return e;
+  const dim3 join(kSplitGroups, (unsigned)up(S::kRows, kThreads / (D / 4)));
+  kv_attention_join_kernel<D, NT><<<join, kThreads, 0, stream>>>(a, p);
+  return hipGetLastError();
+}
+
+// No split where every request's tokens are a step or two of a workgroup's waves.
+bool splits(int64_t max_seq) { return max_seq > 256; }
+
+}  // namespace
+
+int64_t kv_attention_workspace(int64_t T, int64_t Hq, int64_t heads, int64_t D, int64_t B,
+                               int64_t max_query, int64_t max_seq) {
+  (void)T;
+  (void)B;
+  if (!splits(max_seq)) return 0;
+  return partial_bytes(D, row_fragments(max_query * (Hq / heads), D));
+}
+
+hipError_t launch_kv_attention(const AttentionArgs &a, int64_t D, int64_t max_query,
+                               int64_t max_seq, float *workspace, int64_t workspace_bytes,
+                               hipStream_t stream) {
+  const int nt = row_fragments(max_query * a.group, D);
+  const bool split = splits(max_seq) && workspace_bytes >= partial_bytes(D, nt);
+  if (D == 64)
+    return nt == 2 ? launch<64, 2>(a, split, workspace, stream)
+                   : launch<64, 1>(a, split, workspace, stream);
+  if (D == 128)
+    return nt == 2 ? launch<128, 2>(a, split, workspace, stream)
+                   : launch<128, 1>(a, split, workspace, stream);
+  return launch<256, 1>(a, split, workspace, stream);
+}
+
+}  // namespace rfq

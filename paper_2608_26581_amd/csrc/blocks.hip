@@ -1,0 +1,252 @@
+// Block tables and slot maps of a paged key/value cache, from the requests'
+// lengths on the device.
+//
+// With held = ceil(ctx / page), need = ceil((ctx + new) / page) and the exclusive
+// prefix sums F of need - held and S of new over the requests, the n-th new token
+// of request b (row S_b + n) stands at p = ctx_b + n, in block p / page of the
+// request; the block is the table's where p / page < held_b, else the one taken as
+// number F_b + p / page - held_b.  Every taken block holds exactly one new token at
+// its start, so the token with p % page == 0 writes the table entry and nothing
+// is searched twice.
+//
+// The work is two int32 in and a few out per request and two out per token: a few
+// hundred KB at most, so a call costs its launch and its chain of dependent
+// loads.  Every workgroup therefore repeats the prefix sums of all requests
+// (a few values a thread, 16 bytes a request from L2) instead of a second launch
+// that would wait for a first; no workgroup reads what another writes.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <atomic>
+
+#include "kv.h"
+#include "rfq_internal.h"
+
+namespace rfq {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTokensPerGroup = 1024;
+constexpr int kEntriesPerGroup = 1024;
+std::atomic<bool> g_lds_assign[kMaxDevices], g_lds_release[kMaxDevices];
+
+__device__ __forceinline__ int64_t wave_inclusive(int64_t v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t o = __shfl_up(v, d);
+    if (lane >= d) v += o;
+  }
+  return v;
+}
+
+// Exclusive prefix over the workgroup's threads; total: the sum.  part: 4 values
+// of LDS that nothing else uses until the next barrier.
+__device__ __forceinline__ int64_t group_exclusive(int64_t v, int64_t *part, int64_t &total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t incl = wave_inclusive(v);
+  if (lane == 63) part[wave] = incl;
+  __syncthreads();
+  int64_t before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) {
+    if (w < wave) before += part[w];
+    total += part[w];
+  }
+  return before + incl - v;
+}
+
+__device__ __forceinline__ int32_t saturated(int64_t v) {
+  return v > INT32_MAX ? INT32_MAX : (int32_t)v;
+}
+__device__ __forceinline__ int64_t clamped(int64_t v, int64_t lo, int64_t hi) {
+  return v < lo ? lo : (v > hi ? hi : v);
+}
+
+// The last index b in [0, n) with start[b] <= t (start[0] == 0, not decreasing).
+__device__ __forceinline__ int owner(const int32_t *start, int n, int64_t t) {
+  int lo = 0, hi = n;                       // start[lo] <= t, start[hi] > t or hi == n
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (start[mid] <= t) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+__global__ __launch_bounds__(kThreads) void block_assign_kernel(
+    const int32_t *__restrict__ ctx_lens, const int32_t *__restrict__ new_lens, int B,
+    int32_t *tables, int64_t width, const int32_t *__restrict__ free_blocks, int64_t n_free,
+    const int32_t *__restrict__ free_count, int page_shift, int64_t tokens,
+    int32_t *__restrict__ slots, int32_t *__restrict__ positions, int32_t *__restrict__ seq_lens,
+    int32_t *__restrict__ query_starts, int32_t *__restrict__ counts) {
+  extern __shared__ int32_t lds[];
+  int32_t *start = lds;                     // [B] first token of each request
+  int32_t *first = lds + B;                 // [B] blocks taken before it; -1: refused
+  __shared__ int64_t part[3][kThreads / 64];
+  const int tid = threadIdx.x, per = (B + kThreads - 1) / kThreads;
+  const int b0 = tid * per, b1 = min(B, b0 + per);
+  const int64_t page1 = (int64_t(1) << page_shift) - 1;
+  const int64_t count = clamped(free_count[0], 0, n_free);
+
+  auto lengths = [&](int b, int64_t &ctx, int64_t &add, int64_t &held, int64_t &extra,
+                     bool &fits) {
+    ctx = max(ctx_lens[b], 0);
+    add = max(new_lens[b], 0);
+    held = (ctx + page1) >> page_shift;
+    const int64_t need = (ctx + add + page1) >> page_shift;
+    fits = need <= width && ctx + add <= INT32_MAX;
+    extra = fits ? need - held : 0;
+  };
+
+  int64_t ctx, add, held, extra, ntok = 0, nblk = 0, all_tok, all_blk;
+  bool fits;
+  for (int b = b0; b < b1; ++b) {
+    lengths(b, ctx, add, held, extra, fits);
+    ntok += add;
+    nblk += extra;
+  }
+  int64_t s = group_exclusive(ntok, part[0], all_tok);
+  int64_t f = group_exclusive(nblk, part[1], all_blk);
+  // Taken blocks: the requests served form a prefix of those that lack blocks, so
+  // their sum is the largest end of one that is served.
+  int64_t taken = 0;
+  int refused = 0;
+  const bool leader = blockIdx.x == 0;
+  for (int b = b0; b < b1; ++b) {
+    lengths(b, ctx, add, held, extra, fits);
+    const bool ok = fits && (extra == 0 || f + extra <= count);
+    start[b] = saturated(s);
+    first[b] = ok ? saturated(f) : -1;
+    if (ok && extra > 0) taken = f + extra;
+    refused += !ok;
+    if (leader) {
+      query_starts[b] = saturated(s);
+      seq_lens[b] = ok ? (int32_t)(ctx + add) : 0;
+    }
+    s += add;
+    f += extra;
+  }
+  if (leader) {
+    int64_t served = taken, no = refused;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+      const int64_t o = __shfl_xor(served, d);
+      served = o > served ? o : served;
+      no += __shfl_xor(no, d);
+    }
+    if ((tid & 63) == 0) {
+      part[2][tid >> 6] = served;
+      part[0][tid >> 6] = no;               // (part[0] was read before the last barrier)
+    }
+  }
+  __syncthreads();
+  if (leader && tid == 0) {
+    int64_t served = 0, no = 0;
+    for (int w = 0; w < kThreads / 64; ++w) {
+      served = part[2][w] > served ? part[2][w] : served;
+      no += part[0][w];
+    }
+    query_starts[B] = saturated(all_tok);
+    counts[0] = (int32_t)(count - served);
+    counts[1] = saturated(all_tok);
+    counts[2] = (int32_t)no;
+  }
+
+  const int64_t t0 = (int64_t)blockIdx.x * kTokensPerGroup;
+#pragma unroll
+  for (int i = 0; i < kTokensPerGroup / kThreads; ++i) {
+    const int64_t t = t0 + i * kThreads + tid;
+    if (t >= tokens) break;
+    int32_t slot = -1, pos = 0;
+    if (t < all_tok) {
+      const int b = owner(start, B, t);
+      const int64_t c = max(ctx_lens[b], 0), p = c + (t - start[b]);
+      pos = saturated(p);
+      if (first[b] >= 0) {
+        const int64_t had = (c + page1) >> page_shift, j = p >> page_shift;
+        int32_t id;
+        if (j < had) {
+          id = tables[(int64_t)b * width + j];
+        } else {
+          id = free_blocks[count - 1 - (first[b] + (j - had))];
+          if ((p & page1) == 0) tables[(int64_t)b * width + j] = id;
+        }
+        slot = (int32_t)((int64_t)id << page_shift | (p & page1));
+      }
+    }
+    slots[t] = slot;
+    positions[t] = pos;
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void block_release_kernel(
+    const int32_t *__restrict__ lens, const uint8_t *__restrict__ ended, int B,
+    const int32_t *__restrict__ tables, int64_t width, int32_t *__restrict__ free_blocks,
+    int64_t n_free, const int32_t *__restrict__ free_count, int page_shift,
+    int32_t *__restrict__ count_out) {
+  extern __shared__ int32_t lds[];          // [B] blocks given back before each request
+  __shared__ int64_t part[kThreads / 64];
+  const int tid = threadIdx.x, per = (B + kThreads - 1) / kThreads;
+  const int b0 = tid * per, b1 = min(B, b0 + per);
+  const int64_t page1 = (int64_t(1) << page_shift) - 1;
+  const int64_t count = clamped(free_count[0], 0, n_free);
+  auto given = [&](int b) {
+    const int64_t n = (max((int64_t)lens[b], (int64_t)0) + page1) >> page_shift;
+    return ended[b] ? (n < width ? n : width) : (int64_t)0;
+  };
+  int64_t n = 0, all;
+  for (int b = b0; b < b1; ++b) n += given(b);
+  int64_t f = group_exclusive(n, part, all);
+  for (int b = b0; b < b1; ++b) {
+    lds[b] = saturated(f);
+    f += given(b);
+  }
+  __syncthreads();
+  const int64_t room = n_free - count, copied = all < room ? all : room;
+  if (blockIdx.x == 0 && tid == 0) count_out[0] = saturated(count + copied);
+  const int64_t step = (int64_t)gridDim.x * kThreads;
+  for (int64_t k = (int64_t)blockIdx.x * kThreads + tid; k < copied; k += step) {
+    const int b = owner(lds, B, k);
+    free_blocks[count + k] = tables[(int64_t)b * width + (k - lds[b])];
+  }
+}
+
+int log2_of(int page) { return __builtin_ctz((unsigned)page); }
+
+}  // namespace
+
+hipError_t launch_block_assign(const int32_t *ctx, const int32_t *fresh, int B, int32_t *tables,
+                               int64_t width, const int32_t *free_blocks, int64_t n_free,
+                               const int32_t *free_count, int page, int64_t tokens,
+                               int32_t *slots, int32_t *positions, int32_t *seq_lens,
+                               int32_t *query_starts, int32_t *counts, hipStream_t stream) {
+  const int bytes = (int)(2 * sizeof(int32_t) * (B > 0 ? B : 1));
+  const hipError_t e = set_lds_limit(g_lds_assign, (const void *)block_assign_kernel,
+                                     (int)(2 * sizeof(int32_t) * kMaxBlockRequests));
+  if (e != hipSuccess) return e;
+  const int64_t groups = (tokens + kTokensPerGroup - 1) / kTokensPerGroup;
+  block_assign_kernel<<<(unsigned)(groups > 0 ? groups : 1), kThreads, bytes, stream>>>(
+      ctx, fresh, B, tables, width, free_blocks, n_free, free_count, log2_of(page), tokens, slots,
+      positions, seq_lens, query_starts, counts);
+  return hipGetLastError();
+}
+
+hipError_t launch_block_release(const int32_t *lens, const uint8_t *ended, int B,
+                                const int32_t *tables, int64_t width, int32_t *free_blocks,
+                                int64_t n_free, const int32_t *free_count, int page,
+                                int32_t *count_out, hipStream_t stream) {
+  const int bytes = (int)(sizeof(int32_t) * (B > 0 ? B : 1));
+  const hipError_t e = set_lds_limit(g_lds_release, (const void *)block_release_kernel,
+                                     (int)(sizeof(int32_t) * kMaxBlockRequests));
+  if (e != hipSuccess) return e;
+  const int64_t entries = B * width < n_free ? B * width : n_free;
+  int64_t groups = (entries + kEntriesPerGroup - 1) / kEntriesPerGroup;
+  groups = groups < 1 ? 1 : (groups > 256 ? 256 : groups);
+  block_release_kernel<<<(unsigned)groups, kThreads, bytes, stream>>>(
+      lens, ended, B, tables, width, free_blocks, n_free, free_count, log2_of(page), count_out);
+  return hipGetLastError();
+}
+
+}  // namespace rfq

@@ -37,8 +37,33 @@ EXPORTS = (
     "rfq_hif4_gemm_wbf16", "rfq_mfma_fp4_loop", "rfq_mfma_bf16_loop", "rfq_gemm_split",
     "rfq_gemm_workspace_bytes",
     "rfq_gemm_split_noalloc", "rfq_hif4_gemm_split", "rfq_hif4_gemm_workspace_bytes",
+    "rfq_block_assign", "rfq_block_release", "rfq_rope", "rfq_rope_backward", "rfq_kv_append",
+    "rfq_kv_gather", "rfq_kv_attention", "rfq_kv_attention_workspace_bytes",
     "rfq_status_str", "rfq_abi_version",
 )
+
+
+class Heads(ctypes.Structure):
+    """rfq_heads."""
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
+
+
+class RopeSpec(ctypes.Structure):
+    """rfq_rope_spec."""
+    _fields_ = [("positions", ctypes.c_void_p), ("positions_stride", ctypes.c_int64),
+                ("cos_sin", ctypes.c_void_p), ("max_pos", ctypes.c_int64),
+                ("axes", ctypes.c_char_p), ("n_axes", ctypes.c_int32),
+                ("rotary", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
+class KvCacheArgs(ctypes.Structure):
+    """rfq_kv_cache."""
+    _fields_ = [("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p),
+                ("v_codes", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("blocks", ctypes.c_int64), ("heads", ctypes.c_int64), ("page", ctypes.c_int64),
+                ("D", ctypes.c_int64)]
+
 
 # Work items of rfq_mfma_fp4_loop (256 workgroups of 512) and its flops per
 # iteration (each of the 2048 waves issues 8 MFMAs of 32 x 32 x 64).
@@ -105,12 +130,24 @@ def _load():
     lib.rfq_hif4_gemm_split.argtypes = [P, P, P, P, P, P, I64, I64, I64, P, I32, P, I64, P]
     lib.rfq_hif4_gemm_workspace_bytes.argtypes = [I64, I64, I64]
     lib.rfq_hif4_gemm_workspace_bytes.restype = I64
+    H, C, R = ctypes.POINTER(Heads), ctypes.POINTER(KvCacheArgs), ctypes.POINTER(RopeSpec)
+    lib.rfq_block_assign.argtypes = [P, P, I64, P, I64, P, I64, P, I64, I64, P, P, P, P, P, P]
+    lib.rfq_block_release.argtypes = [P, P, I64, P, I64, P, I64, P, I64, P, P]
+    lib.rfq_rope.argtypes = [H, I32, I64, I64, I64, R, H, P]
+    lib.rfq_rope_backward.argtypes = lib.rfq_rope.argtypes
+    lib.rfq_kv_append.argtypes = [H, H, I32, I64, P, C, H, I64, R, H, P]
+    lib.rfq_kv_gather.argtypes = [C, P, I64, P, P, I32, P]
+    lib.rfq_kv_attention.argtypes = [H, I64, I64, C, P, I64, P, P, I64, I64, I64, ctypes.c_float,
+                                     I32, I64, H, P, P, I64, P]
+    lib.rfq_kv_attention_workspace_bytes.argtypes = [I64] * 7
+    lib.rfq_kv_attention_workspace_bytes.restype = I64
     for f in ("rfq_quantize_act", "rfq_quantize_weight", "rfq_gemm", "rfq_dequant",
               "rfq_swiglu_quantize_act", "rfq_gemm_swiglu_quantize", "rfq_gemm_phi",
               "rfq_fallback_map", "rfq_gemm_stream", "rfq_hif4_quantize", "rfq_hif4_dequant",
               "rfq_hif4_gemm", "rfq_hif4_gemm_wbf16", "rfq_mfma_fp4_loop", "rfq_mfma_bf16_loop",
               "rfq_gemm_split", "rfq_hif4_gemm_split",
-              "rfq_gemm_split_noalloc"):
+              "rfq_gemm_split_noalloc", "rfq_block_assign", "rfq_block_release", "rfq_rope",
+              "rfq_rope_backward", "rfq_kv_append", "rfq_kv_gather", "rfq_kv_attention"):
         getattr(lib, f).restype = I32
     _bind_calls(lib)
     lib.rfq_status_str.argtypes = [I32]

@@ -1,0 +1,346 @@
+"""The cache's write and read-back against the oracle's quantizer, and block tables
+and slot maps against plain loops."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_26581_amd as rfq
+import kv_util as ku
+
+pytestmark = pytest.mark.gpu
+
+
+def _dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def _quantized(orc, x):
+    """(codes [T][H][D / 2], scales [T][H][D / 32]) of the oracle."""
+    T, H, D = x.shape
+    c, s = orc.quantize(np.ascontiguousarray(x.reshape(T * H, D)), residual=False)[:2]
+    return c.reshape(T, H, D // 2), s.reshape(T, H, D // 32)
+
+
+def _rows(cache, slots):
+    """The cache's parts at slots, [n][heads][width]."""
+    page = cache[0].shape[2]
+    at = torch.as_tensor(slots).long().cuda()
+    return [p[at // page, :, at % page].cpu().numpy() for p in cache]
+
+
+CASES = [  # T, Hq, heads, D, rotary, axes, interleaved, page
+    (1, 32, 8, 128, 128, 1, False, 16), (1, 1, 1, 64, 32, 2, False, 16),
+    (19, 7, 1, 64, 64, 3, True, 32), (40, 20, 4, 128, 64, 3, False, 64),
+    (33, 8, 8, 256, 256, 1, False, 128), (12, 16, 2, 256, 128, 4, True, 256),
+    (300, 5, 5, 64, 48, 2, False, 16),
+]
+
+
+@pytest.mark.parametrize("T,Hq,heads,D,rotary,axes,interleaved,page", CASES)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_append_matches_the_oracle(orc, T, Hq, heads, D, rotary, axes, interleaved, page, dtype):
+    rng = np.random.default_rng(T + D)
+    print("append T=%d Hq=%d heads=%d D=%d" % (T, Hq, heads, D), flush=True)
+    joint = _dev(rng.standard_normal((T, Hq + 2 * heads, D)).astype(np.float32) *
+                 rng.choice([0.01, 1.0, 30.0], (T, 1, 1)).astype(np.float32)).to(dtype)
+    joint[:, Hq:, :32][::3] = 0                              # blocks of zeros
+    q, k, v = joint[:, :Hq], joint[:, Hq:Hq + heads], joint[:, Hq + heads:]
+    pos = rng.integers(0, 60, (axes, T)).astype(np.int32)
+    cs = ku.table(60, rotary)
+    ax = bytes(int(a) for a in rng.integers(0, axes, rotary // 2))
+    blocks = -(-T // page) + 2
+    slots = rng.permutation(blocks * page)[:T].astype(np.int32)
+    skipped = rng.random(T) < 0.2 if T > 2 else np.zeros(T, bool)
+    slots_in = np.where(skipped, rng.choice([-1, -7, blocks * page, 2 ** 31 - 1], T),
+                        slots).astype(np.int32)
+    cache = rfq.kv_cache(blocks, heads, page, D)
+    for p in cache:
+        p.fill_(0xA5)
+    y = rfq.rfq_kv_append(k, v, _dev(slots_in), cache, q=q, positions=_dev(pos), cos_sin=_dev(cs),
+                          axes=ax, interleaved=interleaved)
+    assert torch.equal(y, rfq.rfq_rope(q, _dev(pos), _dev(cs), ax, interleaved=interleaved))
+    turned = ku.rotate(k.float().cpu().numpy(), pos, cs, ax, interleaved, dtype=np.float32)
+    kc, ks, vc, vs = _rows(cache, slots)
+    keep = ~skipped
+    for got_c, got_s, x in ((kc, ks, turned), (vc, vs, v.float().cpu().numpy())):
+        c, s = _quantized(orc, x.astype(np.float64))
+        assert np.array_equal(got_s[keep], s[keep]) and np.array_equal(got_c[keep], c[keep])
+        assert np.all(got_c[skipped] == 0xA5) and np.all(got_s[skipped] == 0xA5)
+    # Nothing else is written.
+    rest = np.setdiff1d(np.arange(blocks * page), slots[keep])
+    assert all(np.all(r == 0xA5) for r in _rows(cache, rest))
+    for out_dtype in (torch.bfloat16, torch.float32):
+        gk, gv = rfq.rfq_kv_gather(cache, _dev(slots_in), out_dtype)
+        gk, gv = gk.float().cpu().numpy(), gv.float().cpu().numpy()
+        assert np.all(gk[skipped] == 0) and np.all(gv[skipped] == 0)
+        assert np.array_equal(gk[keep], ku.decode(kc, ks)[keep])
+        assert np.array_equal(gv[keep], ku.decode(vc, vs)[keep])
+
+
+def test_append_without_rotation(orc):
+    rng = np.random.default_rng(1)
+    k, v = (rng.standard_normal((9, 2, 128)).astype(np.float32) for _ in range(2))
+    cache = rfq.kv_cache(2, 2, 16, 128)
+    slots = np.arange(20, 29, dtype=np.int32)
+    assert rfq.rfq_kv_append(_dev(k), _dev(v), _dev(slots), cache) is None
+    kc, ks, vc, vs = _rows(cache, slots)
+    for c, s, x in ((kc, ks, k), (vc, vs, v)):
+        want = _quantized(orc, x.astype(np.float64))
+        assert np.array_equal(c, want[0]) and np.array_equal(s, want[1])
+
+
+def test_values_that_are_not_finite():
+    """A block with an infinity or a NaN becomes a NaN block, its neighbours do not; so
+    does a key whose position is outside the table."""
+    x = torch.randn((4, 2, 128), device="cuda")
+    x[0, 1, 40] = float("inf")
+    x[1, 0, 0] = float("nan")
+    x[2, 1, 127] = float("-inf")
+    cache = rfq.kv_cache(1, 2, 16, 128)
+    slots = torch.arange(4, dtype=torch.int32, device="cuda")
+    for dtype in (torch.float32, torch.bfloat16):
+        rfq.rfq_kv_append(x.to(dtype), x.to(dtype), slots, cache)
+        bad = np.zeros((4, 2, 4), bool)
+        bad[0, 1, 1] = bad[1, 0, 0] = bad[2, 1, 3] = True
+        for part in rfq.rfq_kv_gather(cache, slots):
+            assert np.array_equal(np.isnan(part.float().cpu().numpy()), np.repeat(bad, 32, -1))
+    pos = torch.tensor([0, 5, -1, 4], dtype=torch.int32, device="cuda")
+    y = torch.ones((4, 2, 128), device="cuda")
+    rfq.rfq_kv_append(y, y, slots, cache, positions=pos, cos_sin=rfq.rope_table(5, 64))
+    k, v = rfq.rfq_kv_gather(cache, slots)
+    bad = torch.zeros((4, 2, 128), dtype=torch.bool, device="cuda")
+    bad[1:3, :, :64] = True
+    assert torch.equal(k.isnan(), bad) and not v.isnan().any()
+
+
+def test_smallest_and_largest_values(orc):
+    """Subnormal and near-overflow blocks, ties and signed zeros."""
+    rng = np.random.default_rng(2)
+    x = rng.standard_normal((64, 1, 64)).astype(np.float32)
+    x *= np.exp2(rng.integers(-149, 126, (64, 1, 1))).astype(np.float32)
+    x[5] = 0.0
+    x[6, 0, ::2] = -0.0
+    x[7, 0, :8] = [0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0]
+    x[8] = np.float32(3.4028235e38)
+    x[9] = np.float32(1e-45)
+    cache = rfq.kv_cache(4, 1, 16, 64)
+    slots = np.arange(64, dtype=np.int32)
+    rfq.rfq_kv_append(_dev(x), _dev(-x), _dev(slots), cache)
+    kc, ks, vc, vs = _rows(cache, slots)
+    for c, s, y in ((kc, ks, x), (vc, vs, -x)):
+        want = _quantized(orc, y.astype(np.float64))
+        assert np.array_equal(c, want[0]) and np.array_equal(s, want[1])
+
+
+def test_offsets_beyond_32_bits():
+    """Slots whose codes lie past 4 GiB."""
+    heads, page, D = 8, 256, 256
+    blocks = (1 << 32) // (heads * page * D // 2) + 8
+    cache = rfq.kv_cache(blocks, heads, page, D)
+    x = torch.randn((3, heads, D), device="cuda")
+    slots = torch.tensor([blocks * page - 1, (blocks - 3) * page + 5, 0], dtype=torch.int32,
+                         device="cuda")
+    rfq.rfq_kv_append(x, -x, slots, cache)
+    k, v = rfq.rfq_kv_gather(cache, slots)
+    small = rfq.kv_cache(1, heads, 16, D)
+    near = torch.arange(3, dtype=torch.int32, device="cuda")
+    rfq.rfq_kv_append(x, -x, near, small)
+    for a, b in zip((k, v), rfq.rfq_kv_gather(small, near)):
+        assert torch.equal(a, b)
+
+
+def test_append_refusals():
+    x = torch.zeros((4, 2, 128), device="cuda")
+    slots = torch.zeros(4, dtype=torch.int32, device="cuda")
+    cache = rfq.kv_cache(2, 2, 16, 128)
+    pos, cs = torch.zeros(4, dtype=torch.int32, device="cuda"), rfq.rope_table(4, 128)
+    with pytest.raises(ValueError, match="heads"):
+        rfq.rfq_kv_append(x[:, :1], x[:, :1], slots, cache)
+    with pytest.raises(ValueError, match="shape"):
+        rfq.rfq_kv_append(x, x[:3], slots, cache)
+    with pytest.raises(TypeError):
+        rfq.rfq_kv_append(x, x.bfloat16(), slots, cache)
+    with pytest.raises(ValueError, match="slots"):
+        rfq.rfq_kv_append(x, x, slots[:3], cache)
+    with pytest.raises(ValueError, match="positions"):
+        rfq.rfq_kv_append(x, x, slots, cache, q=x)
+    with pytest.raises(ValueError, match="both"):
+        rfq.rfq_kv_append(x, x, slots, cache, positions=pos)
+    with pytest.raises(ValueError, match="without q"):
+        rfq.rfq_kv_append(x, x, slots, cache, q_out=x)
+    with pytest.raises(rfq.RfqError, match="SHAPE"):
+        rfq.rfq_kv_append(x, x, slots, rfq.kv_cache(2, 2, 8, 128))
+    with pytest.raises(ValueError, match="channels"):
+        rfq.rfq_kv_append(x, x, slots, rfq.kv_cache(2, 2, 16, 64))
+    assert rfq.rfq_kv_append(x[:0], x[:0], slots[:0], cache, q=x[:0], positions=pos[:0],
+                             cos_sin=cs).shape == (0, 2, 128)
+    with pytest.raises(TypeError):
+        rfq.rfq_kv_gather(cache, slots, torch.float16)
+
+
+# ---- block tables
+
+def _assign(ctx, new, tables, free, count, page, tokens):
+    """The formula, request by request and token by token."""
+    ctx, new = np.maximum(ctx, 0).astype(np.int64), np.maximum(new, 0).astype(np.int64)
+    B, W = tables.shape
+    tables, count = tables.copy(), min(max(count, 0), len(free))
+    slots, pos = np.full(tokens, -1), np.zeros(tokens, int)
+    seq, starts = np.zeros(B, int), np.zeros(B + 1, int)
+    lack, taken, refused, t = 0, 0, 0, 0
+    for b in range(B):
+        held, need = -(-ctx[b] // page), -(-(ctx[b] + new[b]) // page)
+        starts[b] = t
+        fits = need <= W
+        extra = need - held if fits else 0
+        ok = fits and (extra == 0 or lack + extra <= count)
+        if ok:
+            for j in range(extra):
+                tables[b, held + j] = free[count - 1 - lack - j]
+            taken = max(taken, lack + extra) if extra else taken
+            seq[b] = ctx[b] + new[b]
+        lack += extra
+        refused += not ok
+        for i in range(new[b]):
+            if t < tokens:
+                pos[t] = ctx[b] + i
+                if ok:
+                    slots[t] = tables[b, pos[t] // page] * page + pos[t] % page
+            t += 1
+    starts[B] = t
+    return slots, pos, seq, starts, np.array([count - taken, t, refused]), tables
+
+
+def _tables(rng, ctx, width, page):
+    held = np.minimum(-(-np.maximum(ctx, 0) // page), width)
+    ids = rng.permutation(int(held.sum()) + 50000)
+    tables = np.full((len(ctx), width), -1, np.int32)
+    at = 0
+    for b, h in enumerate(held):
+        tables[b, :h] = ids[at:at + h]
+        at += h
+    return tables, ids[at:].astype(np.int32)
+
+
+@pytest.mark.parametrize("B", [0, 1, 2, 63, 64, 65, 257, 1000, 3000])
+@pytest.mark.parametrize("page", [16, 64, 256])
+@pytest.mark.parametrize("scarce", [False, True])
+def test_assign(B, page, scarce):
+    rng = np.random.default_rng(B + page)
+    ctx = rng.integers(-2, 40 * page // 16, B)
+    ctx[rng.random(B) < 0.2] = page * 2                      # full blocks
+    new = np.where(rng.random(B) < 0.5, 1, rng.integers(-1, 100, B))
+    tables, ids = _tables(rng, ctx, 12, page)
+    total = int(np.maximum(new, 0).sum())
+    lack = int(np.maximum(-(-(np.maximum(ctx, 0) + np.maximum(new, 0)) // page)
+                          - -(-np.maximum(ctx, 0) // page), 0).sum())
+    n_free = max(1, lack // 2 if scarce else lack + 9)
+    free = ids[:n_free + 4]
+    for tokens in (total + 7, total, max(0, total - 3)):
+        args = [np.asarray(a, np.int32) for a in (ctx, new)]
+        t = _dev(tables.reshape(B, 12))
+        got = rfq.rfq_block_assign(_dev(args[0]), _dev(args[1]), t, _dev(free),
+                                   _dev(np.array([n_free], np.int32)), page, tokens)
+        want = _assign(ctx, new, tables, free, n_free, page, total + 7)
+        for name, g, w in zip(("slots", "positions", "seq_lens", "query_starts", "counts"), got, want):
+            w = w[:tokens] if name in ("slots", "positions") else w
+            assert np.array_equal(g.cpu().numpy(), w), name
+        if tokens >= total:
+            assert np.array_equal(t.cpu().numpy(), want[5].reshape(B, 12))
+
+
+def test_assign_count_outside_the_list_and_no_table():
+    ctx, new = np.array([0, 0], np.int32), np.array([20, 40], np.int32)
+    free = np.arange(100, 104, dtype=np.int32)
+    for count in (-3, 0, 3, 4, 1000, 2 ** 31 - 1):
+        for width in (0, 1, 3):
+            tables = np.full((2, width), -1, np.int32)
+            got = rfq.rfq_block_assign(_dev(ctx), _dev(new), _dev(tables), _dev(free),
+                                       _dev(np.array([count], np.int32)), 16, 60)
+            want = _assign(ctx, new, tables, free, count, 16, 60)
+            assert all(np.array_equal(g.cpu().numpy(), w) for g, w in zip(got, want)), (count, width)
+
+
+def test_assign_huge_lengths():
+    """Lengths whose sums pass 32 bits are refused without harm to the others."""
+    big = 2 ** 31 - 1
+    ctx = np.array([5, big, 3, big], np.int32)
+    new = np.array([2, big, 1, 1], np.int32)
+    tables = np.arange(8, dtype=np.int32).reshape(4, 2)
+    s, p, n, q, c = (t.cpu().numpy() for t in rfq.rfq_block_assign(
+        _dev(ctx), _dev(new), _dev(tables), _dev(np.arange(9, dtype=np.int32)),
+        _dev(np.array([9], np.int32)), 16, 10))
+    assert list(n) == [7, 0, 4, 0] and list(c) == [9, big, 2]
+    assert list(s[:2]) == [5, 6] and np.all(s[2:] == -1)
+    assert list(q) == [0, 2, big, big, big] and p[2] == big
+
+
+@pytest.mark.parametrize("B", [0, 1, 64, 300, 2000])
+@pytest.mark.parametrize("room", [0, 3, 100000])
+def test_release(B, room):
+    rng = np.random.default_rng(B + room)
+    page, width = 32, 20
+    lens = rng.integers(-1, width * page + 40, B)
+    ended = (rng.random(B) < 0.4).astype(np.uint8) * rng.integers(1, 256, B).astype(np.uint8)
+    tables = rng.integers(0, 1 << 20, (B, width)).astype(np.int32)
+    back = [tables[b, :min(width, max(0, -(-lens[b] // page)))] for b in range(B) if ended[b]]
+    back = np.concatenate(back) if back else np.zeros(0, np.int32)
+    free = np.full(50 + min(room, len(back) + 5), -9, np.int32)
+    want = free.copy()
+    fit = back[:len(free) - 50]
+    want[50:50 + len(fit)] = fit
+    f = _dev(free)
+    count = rfq.rfq_block_release(_dev(lens.astype(np.int32)), _dev(ended), _dev(tables), f,
+                                  _dev(np.array([50], np.int32)), page)
+    assert count.item() == 50 + len(fit) and np.array_equal(f.cpu().numpy(), want)
+
+
+def test_assign_release_round_trip_in_a_graph():
+    """Steps of decode captured once and replayed: every token of every request has a
+    slot of its own, and all blocks come back."""
+    B, page, blocks = 40, 16, 400
+    free = torch.randperm(blocks, device="cuda").int()
+    tables = torch.full((B, 8), -1, dtype=torch.int32, device="cuda")
+    ctx = torch.zeros(B, dtype=torch.int32, device="cuda")
+    new = torch.ones(B, dtype=torch.int32, device="cuda")
+    count = torch.tensor([blocks], dtype=torch.int32, device="cuda")
+    rfq.rfq_block_assign(ctx, new, tables.clone(), free, count, page, B)      # warm-up
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        slots, _, seq, _, counts = rfq.rfq_block_assign(ctx, new, tables, free, count, page, B)
+        ctx.copy_(seq)
+        count.copy_(counts[:1])
+    seen = []
+    for _ in range(50):
+        g.replay()
+        seen.append(slots.clone())
+    torch.cuda.synchronize()
+    seen = torch.cat(seen)
+    assert seen.min().item() >= 0 and seen.unique().numel() == 50 * B
+    assert count.item() == blocks - 4 * B
+    ended = torch.ones(B, dtype=torch.uint8, device="cuda")
+    back = rfq.rfq_block_release(ctx, ended, tables, free, count, page)
+    assert back.item() == blocks and free.unique().numel() == blocks
+
+
+def test_block_refusals():
+    n = torch.ones(2, dtype=torch.int32, device="cuda")
+    t = torch.zeros((2, 3), dtype=torch.int32, device="cuda")
+    f, c = torch.zeros(4, dtype=torch.int32, device="cuda"), n[:1]
+    with pytest.raises(rfq.RfqError, match="SHAPE"):
+        rfq.rfq_block_assign(n, n, t, f, c, 48, 2)
+    with pytest.raises(ValueError, match="new_lens"):
+        rfq.rfq_block_assign(n, n[:1], t, f, c, 16, 2)
+    with pytest.raises(ValueError, match="block_tables"):
+        rfq.rfq_block_assign(n, n, t[:1], f, c, 16, 2)
+    with pytest.raises(ValueError, match="negative"):
+        rfq.rfq_block_assign(n, n, t, f, c, 16, -1)
+    with pytest.raises(ValueError, match="free_count"):
+        rfq.rfq_block_assign(n, n, t, f, n, 16, 2)
+    with pytest.raises(TypeError):
+        rfq.rfq_block_release(n, n, t, f, c, 16)
+    with pytest.raises(ValueError, match="lens"):
+        rfq.rfq_block_release(t, n.byte(), t, f, c, 16)
+    big = torch.zeros(16385, dtype=torch.int32, device="cuda")
+    with pytest.raises(rfq.RfqError, match="SHAPE"):
+        rfq.rfq_block_assign(big, big, big[:, None], f, c, 16, 2)
