@@ -7,17 +7,45 @@ whose channels are contiguous; tokens and heads may be strided (slices of one
 joint projection).  A cache is a KvCache, or any four tensors of its layout.
 """
 import ctypes
+import threading
 from typing import NamedTuple
 
 import torch
 
+from . import rfq as _binding
 from .rfq import (
-    _FLOAT, _U8, RFQ_BF16, RFQ_F32, Heads, KvCacheArgs, RopeSpec, _check, _dtype_code, _need, _ptr,
-    _stream, load,
+    _FLOAT, _OUT_CODE, _U8, RFQ_BF16, RFQ_F32, Heads, KvCacheArgs, RopeSpec, _check, _dtype_code,
+    _need, _ptr, _result, _stream, load,
 )
 
 _I32 = (torch.int32,)
 _BF16 = (torch.bfloat16,)
+
+# The entry points that the native calls use here, in the order their bind_kv()
+# takes, and the module that has them.
+_NATIVE_ENTRIES = (
+    "rfq_block_assign", "rfq_block_release", "rfq_rope", "rfq_rope_backward", "rfq_kv_append",
+    "rfq_kv_gather", "rfq_kv_attention", "rfq_kv_attention_workspace_bytes",
+)
+_bound = None
+_bind_lock = threading.Lock()
+
+
+def _native(func, *args):
+    """The result of a native call, or None where the Python path takes over."""
+    global _bound
+    calls = _binding._calls
+    if calls is None or _bound is not calls:
+        lib = load()
+        calls = _binding._calls
+        if not calls:
+            return None
+        with _bind_lock:
+            if _bound is not calls:
+                calls.bind_kv(*(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value
+                                for f in _NATIVE_ENTRIES))
+                _bound = calls
+    return _result(func, getattr(calls, func)(*args))
 
 
 class KvCache(NamedTuple):
@@ -121,6 +149,11 @@ def rfq_block_assign(ctx_lens, new_lens, block_tables, free_blocks, free_count, 
     positions [tokens], seq_lens [B], query_starts [B + 1], counts [3]), all int32;
     block_tables [B][width] is updated.  counts: free blocks left, new tokens,
     refused requests."""
+    if stream is None:
+        r = _native("block_assign", ctx_lens, new_lens, block_tables, free_blocks, free_count,
+                    page, tokens)
+        if r is not None:
+            return r
     _need(ctx_lens, "ctx_lens", _I32)
     if ctx_lens.dim() != 1:
         raise ValueError("ctx_lens must be 1-D [B]")
@@ -149,6 +182,10 @@ def rfq_block_assign(ctx_lens, new_lens, block_tables, free_blocks, free_count, 
 def rfq_block_release(lens, ended, block_tables, free_blocks, free_count, page, stream=None):
     """Gives the blocks of the requests with ended != 0 (uint8 [B]) back to the list
     free_blocks (updated) -> its new count [1]."""
+    if stream is None:
+        r = _native("block_release", lens, ended, block_tables, free_blocks, free_count, page)
+        if r is not None:
+            return r
     _need(lens, "lens", _I32)
     if lens.dim() != 1:
         raise ValueError("lens must be 1-D [B]")
@@ -168,6 +205,10 @@ def rfq_block_release(lens, ended, block_tables, free_blocks, free_count, page, 
 
 
 def _rope_call(func, x, positions, cos_sin, axes, interleaved, out, stream):
+    if stream is None:
+        r = _native(func[4:], x, positions, cos_sin, axes, interleaved, out)
+        if r is not None:
+            return r
     _need_heads(x, "x", _FLOAT)
     dev = x.get_device()
     T, H, D = x.shape
@@ -202,6 +243,11 @@ def rfq_kv_append(k, v, slots, cache, q=None, positions=None, cos_sin=None, axes
     """Quantizes k (rotated where positions and cos_sin are given) and v [T][heads][D]
     into the cache's slots [T]; negative slots are skipped.  With q [T][Hq][D]
     returns q rotated (q_out, or a new tensor), else None."""
+    if stream is None:
+        r = _native("kv_append", k, v, slots, *cache, q, positions, cos_sin, axes, interleaved,
+                    q_out)
+        if r is not None:
+            return r[0]
     _need_heads(k, "k", _FLOAT)
     dev = k.get_device()
     T, heads, D = k.shape
@@ -242,6 +288,10 @@ def rfq_kv_append(k, v, slots, cache, q=None, positions=None, cos_sin=None, axes
 def rfq_kv_gather(cache, slots, out_dtype=torch.bfloat16, stream=None):
     """The cached values of slots [n] -> (k, v), each [n][heads][D] (exact in bf16 and
     in fp32); zeros for a slot outside the cache."""
+    if stream is None:
+        r = _native("kv_gather", slots, *cache, _OUT_CODE.get(out_dtype, 2))
+        if r is not None:
+            return r
     _need(slots, "slots", _I32)
     if slots.dim() != 1:
         raise ValueError("slots must be 1-D [n]")
@@ -274,6 +324,12 @@ def rfq_kv_attention(q, cache, block_tables, seq_lens, query_starts, max_query, 
     a request's queries and tokens) divide the work.  scale: 1 / sqrt(D) if None.
     workspace: a contiguous uint8 tensor of rfq_kv_attention_workspace_bytes, or None:
     one from torch's allocator."""
+    if stream is None and isinstance(q, torch.Tensor) and q.dim() == 3 and q.shape[2] > 0:
+        r = _native("kv_attention", q, *cache, block_tables, seq_lens, query_starts, max_query,
+                    max_seq, float(q.shape[2] ** -0.5 if scale is None else scale), causal, window,
+                    return_lse, out, workspace)
+        if r is not None:
+            return r if return_lse else r[0]
     _need_heads(q, "q", _BF16)
     dev = q.get_device()
     T, Hq, D = q.shape

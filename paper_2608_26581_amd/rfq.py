@@ -207,7 +207,11 @@ def _native(func, *args):
         load()
     if not _calls:
         return None
-    r = getattr(_calls, func)(*args)
+    return _result(func, getattr(_calls, func)(*args))
+
+
+def _result(func, r):
+    """What a native call returned, a status raised."""
     if type(r) is int:
         raise RfqError("rfq_" + func, r)
     return r
