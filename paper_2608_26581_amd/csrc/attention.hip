@@ -21,8 +21,6 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include <type_traits>
-
 #include "kv.h"
 #include "mx_device.h"
 #include "rfq_internal.h"
@@ -33,6 +31,9 @@ namespace {
 constexpr int kThreads = 256, kWaves = 4;
 // Workgroups that the split kernel's work is divided over: two per CU.
 constexpr int kSplitGroups = 512;
+// An item's queries, its first loads and the joining of the waves take about as long
+// as this many tiles.
+constexpr int kItemCost = 4;
 constexpr float kLn2 = 0.69314718055994531f;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -62,6 +63,12 @@ __device__ __forceinline__ float across_sum(float v) {
 
 __device__ __forceinline__ uint32_t c_byte(uint32_t w, int i) { return w >> (8 * i) & 0xFFu; }
 
+// Lane `from`'s value in every lane (a scalar).
+__device__ __forceinline__ int64_t lane_value(int64_t v, int from) {
+  return (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)v, from) |
+         (int64_t)__builtin_amdgcn_readlane((int)(v >> 32), from) << 32;
+}
+
 // 8 codes to bf16 times their block's scale.
 __device__ __forceinline__ u32x4 decode_bf16(uint32_t c, float s) {
   u32x4 r;
@@ -70,6 +77,12 @@ __device__ __forceinline__ u32x4 decode_bf16(uint32_t c, float s) {
   r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2));
   r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3));
   return r;
+}
+
+// Orders a wave's LDS accesses (the memory serves them in order).
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
 }
 
 __device__ __forceinline__ v4f mma(const u32x4 &a, const u32x4 &b, const v4f &c) {
@@ -94,6 +107,9 @@ struct Shape {
   static constexpr int kPieces = D == 256 ? 2 : 4;
   static constexpr int kTile = 16 * kPieces;
   static constexpr int kWords = D / 32;                  // code dwords of a lane and token
+  static constexpr int kLoads = kTile * D / 2 / 1024;    // 16-byte loads of a tile's codes
+  static constexpr int kLanes = D / 32;                  // lanes of a token in a load
+  static constexpr int kTokens = 64 / kLanes;            // tokens of a load
   static constexpr int kPitch = 2 * D + 32;              // bytes of a value row in LDS
   static constexpr int kCols = D / 16;                   // 16-channel tiles of O
   static constexpr int kWaveLds = 32 * kPitch;           // >= 16 * D * 4
@@ -106,22 +122,27 @@ struct Request {
 };
 
 template <class S>
-__device__ __forceinline__ Request request(const AttentionArgs &a, int b) {
-  Request r;
-  const int s0 = min(max(a.starts[b], 0), a.T), s1 = min(max(a.starts[b + 1], s0), a.T);
-  r.start = s0;
-  r.nq = s1 - s0;
-  r.len = min(max(a.lens[b], 0), a.capacity);
+__device__ __forceinline__ Request request(const AttentionArgs &a, int start, int nq, int len) {
+  Request r = {start, nq, len};
   int first = 0;
-  if (a.window) first = max(0, r.len - r.nq - a.window + 1);
-  r.tiles0 = min(first, r.len) / S::kTile;
-  r.tiles = max(1, (r.len + S::kTile - 1) / S::kTile - r.tiles0);
-  r.row_tiles = (r.nq * a.group + S::kRows - 1) / S::kRows;
+  if (a.window) first = max(0, len - nq - a.window + 1);
+  r.tiles0 = min(first, len) / S::kTile;
+  r.tiles = max(1, (len + S::kTile - 1) / S::kTile - r.tiles0);
+  r.row_tiles = (nq * a.group + S::kRows - 1) / S::kRows;
   return r;
 }
-// Units of work of a request: token tiles, or with whole items one per (head, row tile).
+template <class S>
+__device__ __forceinline__ Request request(const AttentionArgs &a, int b) {
+  const int s0 = min(max(a.starts[b], 0), a.T), s1 = min(max(a.starts[b + 1], s0), a.T);
+  return request<S>(a, s0, s1 - s0, min(max(a.lens[b], 0), a.capacity));
+}
+// Units of work of an item (a head's row tile of a request): its token tiles and
+// kItemCost for what an item costs besides; without a split one.
+__device__ __forceinline__ int item_units(const Request &r, bool split) {
+  return split ? r.tiles + kItemCost : 1;
+}
 __device__ __forceinline__ int64_t units(const AttentionArgs &a, const Request &r, bool split) {
-  return (int64_t)a.heads * r.row_tiles * (split ? r.tiles : 1);
+  return (int64_t)a.heads * r.row_tiles * item_units(r, split);
 }
 
 // One part of a (request, head, row tile): where its partial result goes.
@@ -131,23 +152,22 @@ struct Partial {
   int4 *item;                             // [groups] item whose first part ends the range
 };
 
-// A lane's codes and scale bytes of a tile of P pieces: token 16 u + lane % 16, channels
-// (lane / 16) D / 4 on.
-template <int D, int P>
+// A lane's part of a tile.  Codes of 1 KB a load, 16 bytes a lane in the order of
+// memory: load i holds token i kTokens + lane / kLanes, block lane % kLanes of it (32
+// channels, one scale byte).  ks: the keys' scale bytes as the operand needs them.
+template <class S>
 struct Codes {
-  using Vec = std::conditional_t<D == 64, u32x2, u32x4>;
-  static constexpr int kVecs = D == 256 ? 2 : 1;
-  Vec k[P][kVecs], v[P][kVecs];
-  uint32_t ks[P], vs[P];                  // D = 256: two bytes
+  u32x4 k[S::kLoads], v[S::kLoads];
+  uint32_t vs[S::kLoads];
+  uint32_t ks[S::kPieces];                // 256 channels: two bytes
 };
 
 template <int D, int NT>
-__global__ __launch_bounds__(kThreads, 2) void kv_attention_kernel(const AttentionArgs a,
+__global__ __launch_bounds__(kThreads, NT == 1 && D <= 128 ? 3 : 2) void kv_attention_kernel(const AttentionArgs a,
                                                                    const Partial part,
                                                                    int split) {
   using S = Shape<D, NT>;
   constexpr int W = S::kWords, P = S::kPieces;
-  using Tile = Codes<D, P>;
   __shared__ alignas(16) uint8_t lds_v[kWaves][S::kWaveLds];
   __shared__ float lds_ml[kWaves][S::kRows][2];
   __shared__ int64_t scan[kWaves];
@@ -158,19 +178,44 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_kernel(const Attenti
   const int col = lane & 15, g = lane >> 4;
   const int wg = blockIdx.x, groups = gridDim.x;
 
-  // This workgroup's range [u0, u1) of the units of all requests.
-  int64_t total = 0, u0, u1, share;
-  {
+  // This workgroup's range [u0, u1) of the units of all requests, and the request b
+  // that u0 is in, whose first unit is base.  A lane holds one request of the 64 from
+  // `held` on.
+  int64_t total = 0, u0, u1, share, base;
+  int b, held = 0;
+  Request mine;
+  auto range = [&] {
+    share = (total + groups - 1) / groups;
+    if (split && share < kWaves + kItemCost) share = kWaves + kItemCost;
+    u0 = share * wg;
+    u1 = u0 + share < total ? u0 + share : total;
+  };
+  auto hold = [&](int from) {
+    held = from;
+    mine = from + lane < a.B ? request<S>(a, from + lane) : Request{};
+  };
+  auto scanned = [&](int64_t n) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int64_t o = __shfl_up(n, d);
+      if (lane >= d) n += o;
+    }
+    return n;
+  };
+  if (a.B <= 64) {
+    hold(0);
+    const int64_t n = units(a, mine, split), incl = scanned(n);
+    total = lane_value(incl, 63);
+    range();
+    const uint64_t at = __ballot(incl - n <= u0 && u0 < incl);
+    b = at ? __builtin_ctzll(at) : 0;
+    base = lane_value(incl - n, b);
+  } else {
     const int per = (a.B + kThreads - 1) / kThreads;
     const int b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
     int64_t n = 0;
-    for (int b = b0; b < b1; ++b) n += units(a, request<S>(a, b), split);
-    int64_t incl = n;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int64_t o = __shfl_up(incl, d);
-      if (lane >= d) incl += o;
-    }
+    for (int i = b0; i < b1; ++i) n += units(a, request<S>(a, i), split);
+    const int64_t incl = scanned(n);
     if (lane == 63) scan[wave] = incl;
     __syncthreads();
     int64_t before = 0;
@@ -179,49 +224,61 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_kernel(const Attenti
       if (w < wave) before += scan[w];
       total += scan[w];
     }
+    total = lane_value(total, 0);
     before += incl - n;
-    share = (total + groups - 1) / groups;
-    if (split && share < kWaves) share = kWaves;
-    u0 = share * wg;
-    u1 = u0 + share < total ? u0 + share : total;
+    range();
     if (u0 < u1 && before <= u0 && u0 < before + n) {
-      int b = b0;
-      for (;; ++b) {
-        const int64_t k = units(a, request<S>(a, b), split);
+      int i = b0;
+      for (;; ++i) {
+        const int64_t k = units(a, request<S>(a, i), split);
         if (u0 < before + k) break;
         before += k;
       }
-      found_b = b;
+      found_b = i;
       found_at = before;
     }
     __syncthreads();
+    b = __builtin_amdgcn_readfirstlane(u0 < u1 ? found_b : 0);
+    base = lane_value(found_at, 0);
+    hold(b);
   }
   if (part.item && tid == 0) part.item[wg] = make_int4(0, 0, 0, 0);
   if (u0 >= u1) return;
-  int b = __builtin_amdgcn_readfirstlane(found_b);
-  int64_t base = found_at;                // first unit of request b
-  Request req = request<S>(a, b);
+  auto pick = [&](int i) {                // request i, of those held
+    if (i >= held + 64) hold(i);
+    const int from = i - held;
+    return request<S>(a, __builtin_amdgcn_readlane(mine.start, from),
+                      __builtin_amdgcn_readlane(mine.nq, from),
+                      __builtin_amdgcn_readlane(mine.len, from));
+  };
+  Request req = pick(b);
 
   uint8_t *vbuf = lds_v[wave];
-  const int lane_bytes = g * (D / 8);     // a lane's codes within a token's
-  const int scale_at = g * (D / 4) / 32;
+  constexpr int L = S::kLoads, LT = S::kLanes;
+  // The 16-byte units of a token's codes in LDS, exchanged so that the 16 tokens of
+  // a piece read theirs from different banks.
+  auto swizzle = [](int token) { return (token / (16 / LT)) & (LT - 1); };
 
   for (int64_t u = u0; u < u1;) {
     int64_t n = units(a, req, split);
     while (u >= base + n) {               // next request that has work
       base += n;
-      req = request<S>(a, ++b);
+      req = pick(++b);
       n = units(a, req, split);
     }
-    const int nk = split ? req.tiles : 1;
+    const int nk = item_units(req, split);
     const int64_t local = u - base;
-    const int item = (int)(local / nk), k0 = (int)(local - (int64_t)item * nk);
+    const int item = local >> 32 ? (int)(local / nk) : (int)((uint32_t)local / (uint32_t)nk);
+    const int k0 = (int)(local - (int64_t)item * nk);
     const int head = item / req.row_tiles, rt = item - head * req.row_tiles;
     const int64_t left = u1 - u;
     const int k1 = (int)(left < nk - k0 ? k0 + left : nk);
-    const int tile0 = req.tiles0 + (split ? k0 : 0);
-    const int tile1 = req.tiles0 + (split ? k1 : req.tiles);
     u += k1 - k0;
+    // The first kItemCost units of an item are no tiles.
+    if (split && k1 <= kItemCost) continue;
+    const bool first = !split || k0 <= kItemCost, complete = first && k1 == nk;
+    const int tile0 = req.tiles0 + (first ? 0 : k0 - kItemCost);
+    const int tile1 = req.tiles0 + (split ? k1 - kItemCost : req.tiles);
 
     // The lane's rows: one of each 16-row tile.
     const int rows = req.nq * a.group, row0 = rt * S::kRows;
@@ -260,72 +317,129 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_kernel(const Attenti
     }
 
     const int32_t *table = a.tables + (int64_t)b * a.width;
-    // The codes of a tile, and which of its 16-token pieces have a block.
-    auto fetch = [&](int tile, Tile &c) -> uint32_t {
-      uint32_t have = 0;
+    // A tile's first rows in the cache, by its pieces, and which of them have a block.
+    int64_t row[P];
+    uint32_t have = 0;
+    auto locate = [&](int tile) {
+      have = 0;
 #pragma unroll
-      for (int s = 0; s < P; ++s) {
-        const int t0 = tile * S::kTile + 16 * s;
+      for (int p = 0; p < P; ++p) {
+        const int t0 = tile * S::kTile + 16 * p;
         int id = -1;
         if (t0 < req.len) id = table[t0 >> a.page_shift];
         const bool ok = (uint32_t)id < (uint32_t)a.blocks;
-        have |= (uint32_t)ok << s;
-        if (!ok) id = 0;
-        const int64_t row =
-            ((((int64_t)id * a.heads + head) << a.page_shift) + (t0 & (a.page - 1))) + col;
-        const uint8_t *kc = a.k_codes + row * (D / 2) + lane_bytes;
-        const uint8_t *vc = a.v_codes + row * (D / 2) + lane_bytes;
-        const uint8_t *ks = a.k_scales + row * (D / 32) + scale_at;
-        const uint8_t *vs = a.v_scales + row * (D / 32) + scale_at;
-        using Vec = typename Tile::Vec;
-#pragma unroll
-        for (int i = 0; i < Tile::kVecs; ++i) {
-          c.k[s][i] = reinterpret_cast<const Vec *>(kc)[i];
-          c.v[s][i] = reinterpret_cast<const Vec *>(vc)[i];
-        }
-        if constexpr (W == 8) {
-          c.ks[s] = *reinterpret_cast<const uint16_t *>(ks);
-          c.vs[s] = *reinterpret_cast<const uint16_t *>(vs);
-        } else {
-          c.ks[s] = *ks;
-          c.vs[s] = *vs;
-        }
+        have |= (uint32_t)ok << p;
+        row[p] = (((int64_t)(ok ? id : 0) * a.heads + head) << a.page_shift) + (t0 & (a.page - 1));
       }
-      return have;
+    };
+    // Load i of a lane, in units of 16 code bytes, so of scale bytes.
+    auto unit_at = [&](int i) -> int64_t {
+      if constexpr (D == 64) return (lane < 32 ? row[2 * i] : row[2 * i + 1]) * LT + (lane & 31);
+      else if constexpr (D == 128) return row[i] * LT + lane;
+      else return row[i / 2] * LT + (i % 2) * 64 + lane;
+    };
+    Codes<S> c;
+    auto fetch_keys = [&] {
+#pragma unroll
+      for (int i = 0; i < L; ++i) c.k[i] = reinterpret_cast<const u32x4 *>(a.k_codes)[unit_at(i)];
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        const uint8_t *ks = a.k_scales + row[p] * LT + col * LT + g * (D / 4) / 32;
+        if constexpr (D == 256) c.ks[p] = *reinterpret_cast<const uint16_t *>(ks);
+        else c.ks[p] = *ks;
+      }
+    };
+    auto fetch_values = [&] {
+#pragma unroll
+      for (int i = 0; i < L; ++i) {
+        c.v[i] = reinterpret_cast<const u32x4 *>(a.v_codes)[unit_at(i)];
+        c.vs[i] = a.v_scales[unit_at(i)];
+      }
     };
 
     // The wave's tiles: every fourth of the range that some row sees.
     int tile = tile0 + wave;
     while (tile < tile1 && (tile + 1) * S::kTile <= any_lo) tile += kWaves;
     const int end = min(tile1, (any_hi + S::kTile) / S::kTile);
-    Tile cur, nxt;
-    uint32_t have = 0, have_nxt = 0;
-    if (tile < end) have = fetch(tile, cur);
+    if (tile < end) {
+      locate(tile);
+      fetch_keys();
+      fetch_values();
+    }
     for (; tile < end; tile += kWaves) {
-      if (tile + kWaves < end) have_nxt = fetch(tile + kWaves, nxt);
+      // Keys to LDS in the order of memory; then the next tile's take their registers.
+      // (The next values follow when this tile's have been decoded.)
+#pragma unroll
+      for (int i = 0; i < L; ++i) {
+        const int token = i * S::kTokens + lane / LT, unit = lane % LT ^ swizzle(token & 15);
+        *reinterpret_cast<u32x4 *>(vbuf + (token * LT + unit) * 16) = c.k[i];
+      }
+      uint32_t ks[P];
+#pragma unroll
+      for (int p = 0; p < P; ++p) ks[p] = c.ks[p];
       const int t0 = tile * S::kTile;
+      const uint32_t held_now = have;
       const bool whole = have == (1u << P) - 1 && t0 >= all_lo && t0 + S::kTile - 1 <= all_hi &&
                          t0 + S::kTile <= req.len;
+      const bool more = tile + kWaves < end;
+      if (more) {
+        locate(tile + kWaves);
+        fetch_keys();
+      }
+      // Keys whose own scale is NaN, or whose values bf16 does not hold, make their
+      // token's scores NaN (values: looked for only where one is in the tile).
+      bool bad[P], odd = false;
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+        odd |= c.vs[i] >= 0xFDu && t0 + i * S::kTokens + lane / LT < req.len;
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+        bad[p] = c_byte(ks[p], 0) == 0xFFu || (D == 256 && c_byte(ks[p], 1) == 0xFFu);
+      if (__any(odd)) {
+#pragma unroll
+        for (int i = 0; i < L; ++i) {
+          // Lanes of token: kLanes neighbours of load i.
+          uint64_t m = __ballot(c.vs[i] >= 0xFDu);
+#pragma unroll
+          for (int p = 0; p < P; ++p) {
+            const int token = 16 * p + col - i * S::kTokens;
+            if (token >= 0 && token < S::kTokens)
+              bad[p] |= (m >> (token * LT) & ((1u << LT) - 1)) != 0;
+          }
+        }
+      }
+      wave_sync();
       // Scores.
       v4f s[NT][P];
 #pragma unroll
       for (int p = 0; p < P; ++p) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) s[t][p] = v4f{0, 0, 0, 0};
-        // A block that is NaN: the keys' own byte 0xFF, or a value byte that bf16 does
-        // not hold; its token's scores become NaN.
-        bool nan = c_byte(cur.ks[p], 0) == 0xFFu || c_byte(cur.vs[p], 0) >= 0xFDu;
-        if constexpr (W == 8)
-          nan = nan || c_byte(cur.ks[p], 1) == 0xFFu || c_byte(cur.vs[p], 1) >= 0xFDu;
+        uint32_t kc[W];
+        const uint8_t *src = vbuf + (16 * p + col) * (D / 2);
+        if constexpr (D == 64) {
+          const u32x2 x = *reinterpret_cast<const u32x2 *>(
+              src + ((g / 2) ^ swizzle(col)) * 16 + (g & 1) * 8);
+          kc[0] = x[0];
+          kc[1] = x[1];
+        } else {
+#pragma unroll
+          for (int w = 0; w < W; w += 4) {
+            const u32x4 x = *reinterpret_cast<const u32x4 *>(
+                src + ((g * (W / 4) + w / 4) ^ swizzle(col)) * 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) kc[w + e] = x[e];
+          }
+        }
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-          const float sc = scale_operand(c_byte(cur.ks[p], w / 4));
-          u32x4 kf = decode_bf16(cur.k[p][w / 4][w % 4], sc);
-          if (w == 0 && nan) kf[0] = 0x7FC07FC0u;
+          u32x4 kf = decode_bf16(kc[w], scale_operand(c_byte(ks[p], w / 4)));
+          if (w == 0 && bad[p]) kf[0] = 0x7FC07FC0u;
 #pragma unroll
           for (int t = 0; t < NT; ++t) s[t][p] = mma(kf, qf[t][w], s[t][p]);
         }
       }
+      wave_sync();
       // Softmax statistics.
       u32x2 pf[NT][P];
 #pragma unroll
@@ -338,7 +452,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_kernel(const Attenti
             float x = s[t][p][i] * a.scale_log2;
             if (!whole) {
               const int tok = t0 + 16 * p + 4 * g + i;
-              const bool see = tok >= lo[t] && tok <= hi[t] && (have >> p & 1);
+              const bool see = tok >= lo[t] && tok <= hi[t] && (held_now >> p & 1);
               x = see ? x : neg_inf();
             }
             s[t][p][i] = x;
@@ -368,23 +482,21 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_kernel(const Attenti
         }
         l[t] += sum;
       }
-      // Values, 32 tokens at a time.
+      // Values, 32 tokens at a time; always finite: a masked token's P is 0 and has to
+      // give 0.
 #pragma unroll
       for (int half = 0; half < P / 2; ++half) {
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          const int p = 2 * half + q;
-          uint8_t *row = vbuf + (16 * q + col) * S::kPitch + g * (D / 2);
+        for (int q = 0; q < D / 64; ++q) {
+          const int i = half * (D / 64) + q;
+          uint8_t *row = vbuf + (q * S::kTokens + lane / LT) * S::kPitch + lane % LT * 64;
+          const float sc = scale_operand(c.vs[i] < 0xFDu ? c.vs[i] : 0u);
 #pragma unroll
-          for (int w = 0; w < W; ++w) {
-            // Always finite: a masked token's P is 0 and has to give 0.
-            const uint32_t byte = c_byte(cur.vs[p], w / 4);
-            *reinterpret_cast<u32x4 *>(row + 16 * w) = decode_bf16(
-                cur.v[p][w / 4][w % 4], scale_operand(byte < 0xFDu ? byte : 0u));
-          }
+          for (int w = 0; w < 4; ++w)
+            *reinterpret_cast<u32x4 *>(row + 16 * w) = decode_bf16(c.v[i][w], sc);
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        if (half == P / 2 - 1 && more) fetch_values();
+        wave_sync();
         const uint8_t *src = vbuf + (4 * g + (col >> 2)) * S::kPitch + (col & 3) * 8;
 #pragma unroll
         for (int c = 0; c < S::kCols; ++c) {
@@ -398,11 +510,8 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_kernel(const Attenti
             o[t][c] = mma(vf, pp, o[t][c]);
           }
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        wave_sync();
       }
-      cur = nxt;
-      have = have_nxt;
     }
 
     // The four waves' results joined, a 16-row tile at a time: each scales its O by
@@ -416,7 +525,6 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_kernel(const Attenti
       }
     }
     __syncthreads();
-    const bool complete = !split || (k0 == 0 && k1 == nk);
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       float top = neg_inf();
@@ -434,7 +542,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_kernel(const Attenti
       __syncthreads();
       const int r = row0 + 16 * t + col;
       const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-      const int slot = 2 * wg + (k0 > 0 ? 0 : 1);
+      const int slot = 2 * wg + (first ? 1 : 0);
       const int i = r / a.group, h = head * a.group + (r - i * a.group);
 #pragma unroll
       for (int c = wave; c < S::kCols; c += kWaves) {
@@ -467,7 +575,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_kernel(const Attenti
       }
       __syncthreads();
     }
-    if (!complete && k0 == 0 && tid == 0) {
+    if (!complete && first && tid == 0) {
       // Its other parts are the first of the following workgroups' ranges.
       const int parts = 1 + (int)((nk - k1 + share - 1) / share);
       part.item[wg] = make_int4(b, head, rt, parts);
@@ -490,19 +598,36 @@ __global__ __launch_bounds__(kThreads) void kv_attention_join_kernel(const Atten
   const int row = blockIdx.y * (kThreads / kLanes) + threadIdx.x / kLanes;
   const int r = it.z * S::kRows + row;
   if (r >= req.nq * a.group) return;
-  const int c = threadIdx.x % kLanes * 4;
-  auto slot = [&](int i) { return (int64_t)(i == 0 ? 2 * wg + 1 : 2 * (wg + i)); };
+  const int lr = threadIdx.x % kLanes, c = 4 * lr;
+  auto slot = [&](int i) { return (int64_t)(i == 0 ? 2 * wg + 1 : 2 * (wg + i)) * S::kRows + row; };
+  // A lane of the row takes every kLanes-th part's statistics.
   float top = neg_inf();
-  for (int i = 0; i < it.w; ++i) top = fmaxf(top, part.ml[(slot(i) * S::kRows + row) * 2]);
+  for (int i = lr; i < it.w; i += kLanes) top = fmaxf(top, part.ml[slot(i) * 2]);
+#pragma unroll
+  for (int d = 1; d < kLanes; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
   const float ref = top == neg_inf() ? 0.0f : top;
   float sum = 0.0f;
   v4f x = {0, 0, 0, 0};
-  for (int i = 0; i < it.w; ++i) {
-    const float *ml = part.ml + (slot(i) * S::kRows + row) * 2;
-    const float f = exp2_hw(ml[0] - ref);
-    sum += ml[1] * f;
-    x += *reinterpret_cast<const v4f *>(part.o + (slot(i) * S::kRows + row) * D + c) * f;
+  for (int i0 = 0; i0 < it.w; i0 += kLanes) {
+    float f = 0.0f;
+    if (i0 + lr < it.w) {
+      const float *ml = part.ml + slot(i0 + lr) * 2;
+      f = exp2_hw(ml[0] - ref);
+      sum += ml[1] * f;
+    }
+    constexpr int kBatch = 8;                            // loads in flight
+    for (int i = 0; i < min(kLanes, it.w - i0); i += kBatch) {
+      v4f y[kBatch];
+#pragma unroll
+      for (int e = 0; e < kBatch; ++e)
+        y[e] = *reinterpret_cast<const v4f *>(part.o + slot(min(i0 + i + e, it.w - 1)) * D + c);
+#pragma unroll
+      for (int e = 0; e < kBatch; ++e)
+        if (i0 + i + e < it.w) x += y[e] * __shfl(f, i + e, kLanes);
+    }
   }
+#pragma unroll
+  for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor(sum, d);
   x *= sum == 0.0f ? 0.0f : 1.0f / sum;
   const int i = r / a.group, h = it.y * a.group + (r - i * a.group);
   const bf16x4 y = {(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
