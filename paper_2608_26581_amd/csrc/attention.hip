@@ -21,81 +21,18 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "attention_device.h"
 #include "kv.h"
-#include "mx_device.h"
 #include "rfq_internal.h"
 
 namespace rfq {
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4;
 // Workgroups that the split kernel's work is divided over: two per CU.
 constexpr int kSplitGroups = 512;
 // An item's queries, its first loads and the joining of the waves take about as long
 // as this many tiles.
 constexpr int kItemCost = 4;
-constexpr float kLn2 = 0.69314718055994531f;
-
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef float v4f __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-
-__device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
-__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// Maximum / sum over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
-__device__ __forceinline__ float across_max(float v) {
-  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-__device__ __forceinline__ float across_sum(float v) {
-  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-  auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
-}
-
-__device__ __forceinline__ uint32_t c_byte(uint32_t w, int i) { return w >> (8 * i) & 0xFFu; }
-
-// Lane `from`'s value in every lane (a scalar).
-__device__ __forceinline__ int64_t lane_value(int64_t v, int from) {
-  return (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)v, from) |
-         (int64_t)__builtin_amdgcn_readlane((int)(v >> 32), from) << 32;
-}
-
-// 8 codes to bf16 times their block's scale.
-__device__ __forceinline__ u32x4 decode_bf16(uint32_t c, float s) {
-  u32x4 r;
-  r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0));
-  r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1));
-  r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2));
-  r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3));
-  return r;
-}
-
-// Orders a wave's LDS accesses (the memory serves them in order).
-__device__ __forceinline__ void wave_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
-__device__ __forceinline__ v4f mma(const u32x4 &a, const u32x4 &b, const v4f &c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
-                                                 __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-
-// Element i of lane l: 16-bit element (l mod 16) of row 4 (l / 16) + i, each lane
-// pointing at 4 elements: lanes 4 j .. 4 j + 3 of a group of 16 at its row j.
-__device__ __forceinline__ u32x2 read_transposed(const uint8_t *p) {
-  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p));
-}
 
 // ---- the shapes and the requests
 
@@ -115,33 +52,13 @@ struct Shape {
   static constexpr int kWaveLds = 32 * kPitch;           // >= 16 * D * 4
 };
 
-struct Request {
-  int start, nq, len;
-  int tiles0, tiles;                      // first token tile that a row sees; number (>= 1)
-  int row_tiles;
-};
-
-template <class S>
-__device__ __forceinline__ Request request(const AttentionArgs &a, int start, int nq, int len) {
-  Request r = {start, nq, len};
-  int first = 0;
-  if (a.window) first = max(0, len - nq - a.window + 1);
-  r.tiles0 = min(first, len) / S::kTile;
-  r.tiles = max(1, (len + S::kTile - 1) / S::kTile - r.tiles0);
-  r.row_tiles = (nq * a.group + S::kRows - 1) / S::kRows;
-  return r;
-}
-template <class S>
-__device__ __forceinline__ Request request(const AttentionArgs &a, int b) {
-  const int s0 = min(max(a.starts[b], 0), a.T), s1 = min(max(a.starts[b + 1], s0), a.T);
-  return request<S>(a, s0, s1 - s0, min(max(a.lens[b], 0), a.capacity));
-}
 // Units of work of an item (a head's row tile of a request): its token tiles and
 // kItemCost for what an item costs besides; without a split one.
 __device__ __forceinline__ int item_units(const Request &r, bool split) {
   return split ? r.tiles + kItemCost : 1;
 }
 __device__ __forceinline__ int64_t units(const AttentionArgs &a, const Request &r, bool split) {
+  if (r.nq * a.group > a.most_rows) return 0;
   return (int64_t)a.heads * r.row_tiles * item_units(r, split);
 }
 
@@ -670,22 +587,44 @@ hipError_t launch(const AttentionArgs &a, bool split, float *work, hipStream_t s
   return hipGetLastError();
 }
 
+// Requests up to this many rows (queries times group) never take the wide kernel.
+constexpr int kFewRows = 64;
+constexpr int64_t kWideTiles = 128;
+
 // No split where every request's tokens are a step or two of a workgroup's waves.
 bool splits(int64_t max_seq) { return max_seq > 256; }
+
+// Whether requests with many rows take the wide kernel: it does not split tokens, so its
+// row tiles alone have to fill the GPU (and fit a launch).
+bool wide_applies(int64_t T, int64_t group, int64_t heads, int64_t B, int64_t max_query) {
+  const int64_t tiles = T * group / 128 * heads;
+  return max_query * group > kFewRows && tiles >= kWideTiles &&
+         tiles + B * heads <= UINT32_MAX / kThreads;
+}
 
 }  // namespace
 
 int64_t kv_attention_workspace(int64_t T, int64_t Hq, int64_t heads, int64_t D, int64_t B,
                                int64_t max_query, int64_t max_seq) {
-  (void)T;
-  (void)B;
   if (!splits(max_seq)) return 0;
+  if (wide_applies(T, Hq / heads, heads, B, max_query)) {
+    if (B == 1) return 0;
+    max_query = kFewRows;
+  }
   return partial_bytes(D, row_fragments(max_query * (Hq / heads), D));
 }
 
-hipError_t launch_kv_attention(const AttentionArgs &a, int64_t D, int64_t max_query,
+hipError_t launch_kv_attention(const AttentionArgs &args, int64_t D, int64_t max_query,
                                int64_t max_seq, float *workspace, int64_t workspace_bytes,
                                hipStream_t stream) {
+  AttentionArgs a = args;
+  a.most_rows = INT32_MAX;
+  if (wide_applies(a.T, a.group, a.heads, a.B, max_query)) {
+    a.most_rows = a.B == 1 ? 0 : kFewRows;
+    const hipError_t e = launch_kv_attention_wide(a, D, a.most_rows, stream);
+    if (e != hipSuccess || a.B == 1) return e;
+    max_query = (kFewRows + a.group - 1) / a.group;
+  }
   const int nt = row_fragments(max_query * a.group, D);
   const bool split = splits(max_seq) && workspace_bytes >= partial_bytes(D, nt);
   if (D == 64)

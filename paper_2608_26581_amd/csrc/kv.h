@@ -47,6 +47,7 @@ struct AttentionArgs {
   int64_t width;
   int32_t T, Hq, heads, group, blocks, page, page_shift, B;
   int32_t capacity;                 // tokens a table row can name
+  int32_t most_rows;                // requests with more are another launch's
   int32_t causal;
   int32_t window;                   // 0: none
   float scale_log2;                 // scale * log2(e)
@@ -56,6 +57,9 @@ struct AttentionArgs {
 };
 int64_t kv_attention_workspace(int64_t T, int64_t Hq, int64_t heads, int64_t D, int64_t B,
                                int64_t max_query, int64_t max_seq);
+// The wide kernel: requests with more than few_rows rows (queries times group).
+hipError_t launch_kv_attention_wide(const AttentionArgs &args, int64_t D, int few_rows,
+                                    hipStream_t stream);
 hipError_t launch_kv_attention(const AttentionArgs &args, int64_t D, int64_t max_query,
                                int64_t max_seq, float *workspace, int64_t workspace_bytes,
                                hipStream_t stream);
