@@ -49,15 +49,17 @@ struct Wide {
 
 // Requests with more than few_rows rows (the others are attention.hip's).  The row
 // tiles of request b are numbered from floor(start_b group / 128) + b, which leaves
-// room for every row.  Two tile buffers: while one is multiplied the next is decoded
-// into the other from registers, which the loads of the one after then take.
+// room for every row.  Matrix and vector units run side by side: a wave's step k does
+// the softmax of tile k, whose scores it has, the scores of tile k + 1 in the registers
+// that each half of it leaves, and O += V P of tile k with the decoding of keys k + 2 and
+// values k + 1 into the LDS buffers that step k - 1 left.  One barrier a step.
 template <int D>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void kv_attention_wide_kernel(
     const AttentionArgs a, int few_rows, int tiles) {
   using S = Wide<D>;
   constexpr int LT = S::kLanes, KS = D / 16, CT = D / 32, L = S::kLoads;
-  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];   // [2][keys, values]
-  __shared__ int lds_have[2][S::kTile / 16];              // whether a piece has a block
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];   // [2] keys, [2] values
+  __shared__ int lds_have[4][S::kTile / 16];              // whether a piece has a block
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, h = lane >> 5;
@@ -112,8 +114,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void kv_attention_wide_
 
   const int32_t *table = a.tables + (int64_t)b * a.width;
   // The thread's blocks of a tile: number n = tid + 256 l, block n % LT of token n / LT.
+  // Scale bytes of both come with the keys; the values follow a step later.
   u32x4 kc[L], vc[L];
-  uint32_t ks[L], vs[L];
+  uint32_t ks[L], vs[L], vs_next[L];
+  int64_t at[L];
   int id[L], ok[L];
   auto look_up = [&](int tile) {
 #pragma unroll
@@ -123,41 +127,57 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void kv_attention_wide_
       if (tid + kThreads * l < S::kBlocks && t < req.len) id[l] = table[t >> a.page_shift];
     }
   };
-  auto fetch = [&](int tile) {
+  auto fetch_keys = [&](int tile) {
 #pragma unroll
     for (int l = 0; l < L; ++l) {
       const int n = tid + kThreads * l, t = tile * S::kTile + n / LT;
       ok[l] = (uint32_t)id[l] < (uint32_t)a.blocks;
-      if (n < S::kBlocks) {
-        const int64_t row =
-            (((int64_t)(ok[l] ? id[l] : 0) * a.heads + head) << a.page_shift) + (t & (a.page - 1));
-        const int64_t at = row * LT + n % LT;
-        kc[l] = reinterpret_cast<const u32x4 *>(a.k_codes)[at];
-        vc[l] = reinterpret_cast<const u32x4 *>(a.v_codes)[at];
-        ks[l] = a.k_scales[at];
-        vs[l] = a.v_scales[at];
-      }
+      const int64_t row =
+          (((int64_t)(ok[l] ? id[l] : 0) * a.heads + head) << a.page_shift) + (t & (a.page - 1));
+      at[l] = row * LT + n % LT;
+      kc[l] = reinterpret_cast<const u32x4 *>(a.k_codes)[at[l]];
+      ks[l] = a.k_scales[at[l]];
+      vs_next[l] = a.v_scales[at[l]];
     }
   };
-  auto decode = [&](int buf) {
-    uint8_t *keys = lds + buf * 2 * S::kPart, *vals = keys + S::kPart;
+  auto fetch_values = [&] {
+#pragma unroll
+    for (int l = 0; l < L; ++l) {
+      vc[l] = reinterpret_cast<const u32x4 *>(a.v_codes)[at[l]];
+      vs[l] = vs_next[l];
+    }
+  };
+  // A block that is NaN (a value byte that bf16 does not hold) makes its token's scores
+  // NaN; the values in LDS are finite, so that a masked P gives 0.
+  auto decode_keys = [&](int tile) {
+    uint8_t *keys = lds + (tile & 1) * S::kPart;
 #pragma unroll
     for (int l = 0; l < L; ++l) {
       const int n = tid + kThreads * l, token = n / LT, block = n % LT;
-      if (n < S::kBlocks) {
-        if (n % (16 * LT) == 0) lds_have[buf][token / 16] = ok[l];
-        // A block that is NaN (a value byte that bf16 does not hold) makes its token's
-        // scores NaN; the values in LDS are finite, so that a masked P gives 0.
-        const bool nan = ks[l] == 0xFFu || vs[l] >= 0xFDu;
-        const float sk = scale_operand(ks[l]), sv = scale_operand(vs[l] < 0xFDu ? vs[l] : 0u);
+      if (S::kBlocks % kThreads == 0 || n < S::kBlocks) {
+        if (n % (16 * LT) == 0) lds_have[tile & 3][token / 16] = ok[l];
+        const bool nan = ks[l] == 0xFFu || vs_next[l] >= 0xFDu;
+        const float sk = scale_operand(ks[l]);
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           u32x4 x = decode_bf16(kc[l][w], sk);
           if (w == 0 && nan) x[0] = 0x7FC07FC0u;
           *reinterpret_cast<u32x4 *>(keys + S::key(token, 4 * block + w)) = x;
+        }
+      }
+    }
+  };
+  auto decode_values = [&](int tile) {
+    uint8_t *vals = lds + (2 + (tile & 1)) * S::kPart;
+#pragma unroll
+    for (int l = 0; l < L; ++l) {
+      const int n = tid + kThreads * l, token = n / LT, block = n % LT;
+      if (S::kBlocks % kThreads == 0 || n < S::kBlocks) {
+        const float sv = scale_operand(vs[l] < 0xFDu ? vs[l] : 0u);
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
           *reinterpret_cast<u32x4 *>(vals + S::value(token, 2 * block + w / 2) + 16 * (w % 2)) =
               decode_bf16(vc[l][w], sv);
-        }
       }
     }
   };
@@ -166,95 +186,123 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void kv_attention_wide_
 #pragma unroll
   for (int t = 0; t < CT; ++t) o[t] = v16f{};
   float m = neg_inf(), sum = 0.0f;                        // m: in units of log2
+  // Whether some row of the wave sees something of a tile.
+  auto seen = [&](int tile) {
+    return tile < end && tile * S::kTile <= any_hi && (tile + 1) * S::kTile > any_lo;
+  };
+  v16f s[2];
+  // Half t of a tile's scores.
+  auto score = [&](int tile, int t) {
+    const uint8_t *keys = lds + (tile & 1) * S::kPart;
+    s[t] = v16f{};
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+      s[t] = mma32(*reinterpret_cast<const u32x4 *>(keys + S::key(32 * t + col, 2 * k + h)), qf[k],
+                   s[t]);
+  };
 
   if (tile0 < end) {
     look_up(tile0);
-    fetch(tile0);
-    if (tile0 + 1 < end) look_up(tile0 + 1);
-    decode(0);
-    if (tile0 + 1 < end) fetch(tile0 + 1);
-    if (tile0 + 2 < end) look_up(tile0 + 2);
+    fetch_keys(tile0);
+    fetch_values();
+    look_up(tile0 + 1);
+    decode_keys(tile0);
+    fetch_keys(tile0 + 1);
+    look_up(tile0 + 2);
+    decode_values(tile0);
+    fetch_values();
+    decode_keys(tile0 + 1);
+    fetch_keys(tile0 + 2);
+    look_up(tile0 + 3);
+    __syncthreads();
+    score(tile0, 0);
+    score(tile0, 1);
   }
   for (int tile = tile0; tile < end; ++tile) {
-    const int buf = (tile - tile0) & 1;
-    __syncthreads();
-    if (tile + 1 < end) {
-      decode(buf ^ 1);
-      if (tile + 2 < end) fetch(tile + 2);
-      if (tile + 3 < end) look_up(tile + 3);
-    }
     const int t0 = tile * S::kTile;
-    if (t0 > any_hi || t0 + S::kTile <= any_lo) continue;
-    const uint8_t *keys = lds + buf * 2 * S::kPart, *vals = keys + S::kPart;
-    v16f s[2] = {v16f{}, v16f{}};
+    const bool now = seen(tile);
+    if (now) {
+      int have[4];
 #pragma unroll
-    for (int k = 0; k < KS; ++k) {
+      for (int p = 0; p < 4; ++p) have[p] = lds_have[tile & 3][p];
+      const bool whole = (have[0] & have[1] & have[2] & have[3]) && t0 >= all_lo &&
+                         t0 + S::kTile - 1 <= all_hi;
+      if (!__builtin_amdgcn_readfirstlane(whole)) {
+        asm volatile("");                                 // (a branch, not selects)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int tok = t0 + 32 * t + 8 * (e / 4) + 4 * h + e % 4;
+            const bool see = tok >= lo && tok <= hi && have[2 * t + e / 8];
+            s[t][e] = see ? s[t][e] : neg_inf();
+          }
+      }
+      float top = s[0][0];
 #pragma unroll
       for (int t = 0; t < 2; ++t)
-        s[t] = mma32(*reinterpret_cast<const u32x4 *>(keys + S::key(32 * t + col, 2 * k + h)),
-                     qf[k], s[t]);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][e]);
+      const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top),
+                                                         __float_as_uint(top), false, false);
+      top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * c;
+      // The reference follows the maximum only where P would pass 2^8.
+      if (__any(top > m + 8.0f)) {
+        asm volatile("");
+        const float up = fmaxf(top, m);
+        const float f = exp2_hw(m - (up == neg_inf() ? 0.0f : up));
+        sum *= f;
+#pragma unroll
+        for (int t = 0; t < CT; ++t) o[t] *= f;
+        m = up;
+      }
     }
-    int have[4];
-#pragma unroll
-    for (int p = 0; p < 4; ++p) have[p] = lds_have[buf][p];
-    const bool whole = (have[0] & have[1] & have[2] & have[3]) && t0 >= all_lo &&
-                       t0 + S::kTile - 1 <= all_hi;
-    if (!whole) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int tok = t0 + 32 * t + 8 * (e / 4) + 4 * h + e % 4;
-          const bool see = tok >= lo && tok <= hi && have[2 * t + e / 8];
-          s[t][e] = see ? s[t][e] : neg_inf();
-        }
-    }
-    float top = s[0][0];
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][e]);
-    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top),
-                                                       false, false);
-    top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * c;
-    // The reference follows the maximum only where P would pass 2^8.
-    if (__any(top > m + 8.0f)) {
-      const float next = fmaxf(top, m), ref = next == neg_inf() ? 0.0f : next;
-      const float f = exp2_hw(m - ref);
-      sum *= f;
-#pragma unroll
-      for (int t = 0; t < CT; ++t) o[t] *= f;
-      m = next;
-    }
-    const float ref = m == neg_inf() ? 0.0f : m;
     u32x2 pf[2][4];
+    const float ref = m == neg_inf() ? 0.0f : m;
+    auto weigh = [&](int t, int q) {
+      float e[4];
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+      for (int x = 0; x < 4; ++x) {
+        e[x] = exp2_hw(__builtin_fmaf(s[t][4 * q + x], c, -ref));
+        sum += e[x];
+      }
+      const bf16x4 y = {(__bf16)e[0], (__bf16)e[1], (__bf16)e[2], (__bf16)e[3]};
+      pf[t][q] = __builtin_bit_cast(u32x2, y);
+    };
+    if (now) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float e[4];
+      for (int q = 0; q < 4; ++q) weigh(0, q);
+      score(tile + 1, 0);
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          e[x] = exp2_hw(__builtin_fmaf(s[t][4 * q + x], c, -ref));
-          sum += e[x];
+      for (int q = 0; q < 4; ++q) weigh(1, q);
+      score(tile + 1, 1);
+      const uint8_t *vals = lds + (2 + (tile & 1)) * S::kPart;
+      // Tokens 16 u + 4 h + 0..3 and + 8 of it: the order in which P holds them.
+      const int l16 = lane & 15, half = lane >> 4 & 1;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const u32x4 p = {pf[u / 2][u % 2 * 2][0], pf[u / 2][u % 2 * 2][1],
+                         pf[u / 2][u % 2 * 2 + 1][0], pf[u / 2][u % 2 * 2 + 1][1]};
+        const int token = 16 * u + 4 * h + (l16 >> 2);
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+          const u32x2 v0 = read_transposed(vals + S::value(token, 2 * t + half) + (l16 & 3) * 8);
+          const u32x2 v1 =
+              read_transposed(vals + S::value(token + 8, 2 * t + half) + (l16 & 3) * 8);
+          o[t] = mma32(u32x4{v0[0], v0[1], v1[0], v1[1]}, p, o[t]);
         }
-        const bf16x4 y = {(__bf16)e[0], (__bf16)e[1], (__bf16)e[2], (__bf16)e[3]};
-        pf[t][q] = __builtin_bit_cast(u32x2, y);
       }
-    // Tokens 16 u + 4 h + 0..3 and + 8 of it: the order in which P holds them.
-    const int l16 = lane & 15, half = lane >> 4 & 1;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const u32x4 p = {pf[u / 2][u % 2 * 2][0], pf[u / 2][u % 2 * 2][1],
-                       pf[u / 2][u % 2 * 2 + 1][0], pf[u / 2][u % 2 * 2 + 1][1]};
-      const int token = 16 * u + 4 * h + (l16 >> 2);
-#pragma unroll
-      for (int t = 0; t < CT; ++t) {
-        const u32x2 v0 = read_transposed(vals + S::value(token, 2 * t + half) + (l16 & 3) * 8);
-        const u32x2 v1 = read_transposed(vals + S::value(token + 8, 2 * t + half) + (l16 & 3) * 8);
-        o[t] = mma32(u32x4{v0[0], v0[1], v1[0], v1[1]}, p, o[t]);
-      }
+    } else {
+      score(tile + 1, 0);
+      score(tile + 1, 1);
     }
+    // (Tiles past the end are decoded and scored too: from places that exist, not used.)
+    decode_values(tile + 1);
+    fetch_values();
+    decode_keys(tile + 2);
+    fetch_keys(tile + 3);
+    look_up(tile + 4);
+    __syncthreads();
   }
 
   const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum),

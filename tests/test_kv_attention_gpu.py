@@ -80,6 +80,53 @@ def test_prompts(D, nq, extra, causal):
     _check(rng, [(nq + extra, nq)], 4, 1, D, 64, causal=causal)
 
 
+# Enough row tiles that requests of more than a few rows take the kernel of 128-row
+# workgroups: 64 heads with two queries each, about 150 rows of q.
+WIDE = [[(150, 150)], [(171, 70), (64, 64), (33, 1), (90, 40)], [(40, 40), (0, 0), (2, 2), (129, 128)],
+        [(65, 64), (0, 3), (20, 90)]]
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("reqs", WIDE)
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 1), (True, 37), (False, 70)])
+def test_many_rows(D, reqs, causal, window):
+    rng = np.random.default_rng(D + window)
+    _check(rng, reqs, 128, 64, D, 16, causal=causal, window=window)
+
+
+@pytest.mark.parametrize("group,heads,page", [(1, 128, 32), (3, 48, 128), (7, 20, 64), (20, 8, 256)])
+def test_many_rows_groups(group, heads, page):
+    rng = np.random.default_rng(group)
+    _check(rng, [(200, 110), (70, 40)], group * heads, heads, 64, page)
+
+
+@pytest.mark.parametrize("scale", [25.0, -0.7, 0.0])
+def test_many_rows_scale(scale):
+    rng = np.random.default_rng(17)
+    _check(rng, [(180, 130), (20, 20)], 128, 64, 64, 16, scale=scale)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_many_rows_missing_and_nan_blocks(D):
+    """Table entries outside the cache, and NaN blocks reaching only rows that attend."""
+    rng = np.random.default_rng(18)
+    reqs = [(220, 130), (60, 20)]
+    cache = ku.Cache(rng, [n for n, _ in reqs], 64, 16, D)
+    cache.tables[0, 2] = -1
+    cache.tables[0, 11:13] = 2 ** 31 - 1
+    for token, part, head in ((100, 1, 3), (160, 3, 7), (170, 3, 3), (30, 1, 9)):
+        cache.parts[part][cache.tables[0, token // 16], head, token % 16, D // 64] = 255
+    q = _queries(rng, 150, 128, D)
+    for window in (0, 60):
+        out, lse = _run(q, cache, reqs, window=window)
+        ref = ku.attention(q, cache, [n for n, _ in reqs], _starts(reqs), D ** -0.5, True, window)
+        nan = np.isnan(ref[0]).any(-1)
+        got = out.float().cpu().numpy()
+        assert np.array_equal(np.isnan(got).all(-1), nan) and np.array_equal(np.isnan(got).any(-1), nan)
+        tol = (2.0 ** -8 + 2.0 ** -15 * ref[3][..., None]) * ref[2] + 2.0 ** -8 * np.abs(ref[0])
+        assert np.all((np.abs(got - ref[0]) <= tol)[~nan])
+
+
 def test_long_prompt_over_many_workgroups():
     """Enough rows that the row tiles alone fill the GPU."""
     rng = np.random.default_rng(5)
