@@ -13,6 +13,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "attention_device.h"
 #include "kv.h"
@@ -28,38 +29,42 @@ __device__ __forceinline__ v16f mma32(const u32x4 &a, const u32x4 &b, const v16f
                                                  __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-template <int D>
+template <int D, int NR, int WAVES>
 struct Wide {
-  static constexpr int kRows = 128, kTile = 64, kWaveRows = 32;
+  static constexpr int kThreads = 64 * WAVES;
+  static constexpr int kWaveRows = 32 * NR, kRows = WAVES * kWaveRows, kTile = 64;
   static constexpr int kLanes = D / 32;                   // 32-channel blocks of a token
   static constexpr int kBlocks = kTile * kLanes;          // of a tile
   static constexpr int kLoads = (kBlocks + kThreads - 1) / kThreads;
-  static constexpr int kPart = kTile * 2 * D;             // bytes of a tile's keys (values)
-  static constexpr int kLds = 4 * kPart;                  // two tiles
-  // Rows of 2 D bytes.  Keys in units of 16 bytes (an operand's 8 channels), values in
-  // units of 32 (the 16 channels that a transposing read takes), exchanged by the
-  // token so that the rows that are read at once lie in different banks.
-  static __device__ __forceinline__ int key(int token, int unit) {
-    return token * 2 * D + (unit ^ (D == 64 ? token >> 1 & 7 : token & 15)) * 16;
-  }
-  static __device__ __forceinline__ int value(int token, int unit) {
-    return token * 2 * D + (unit ^ (D == 64 ? token >> 1 & 3 : token & 7)) * 32;
-  }
+  // Rows in LDS are padded so that what 16 lanes read or write at once lies in
+  // different banks (at 128 channels; nearly so at 64 and 256): 16 bytes of 16 tokens (the
+  // keys' operand), 64 bytes of 4 neighbouring tokens (what transposing reads of the
+  // values take), and 16 bytes of every block of some tokens when either is written.  All
+  // addresses are then one of four registers and a constant.
+  static constexpr int kKeyPitch = 2 * D + 16, kValuePitch = 2 * D + 80;
+  static constexpr int kKeys = kTile * kKeyPitch, kValues = kTile * kValuePitch;
+  static constexpr int kLds = 2 * (kKeys + kValues);      // two tiles
 };
 
 // Requests with more than few_rows rows (the others are attention.hip's).  The row
 // tiles of request b are numbered from floor(start_b group / 128) + b, which leaves
-// room for every row.  Matrix and vector units run side by side: a wave's step k does
-// the softmax of tile k, whose scores it has, the scores of tile k + 1 in the registers
-// that each half of it leaves, and O += V P of tile k with the decoding of keys k + 2 and
-// values k + 1 into the LDS buffers that step k - 1 left.  One barrier a step.
-template <int D>
-__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void kv_attention_wide_kernel(
+// room for every row.
+//
+// Matrix and vector units run side by side: in a step, half a tile of 32 tokens, a wave
+// turns its scores S_j into P_j while the matrix cores compute S_(j+1) and add
+// P_(j-1) V to O; the three are independent.  Their operands are read from LDS two
+// products ahead.  In a tile's second half the keys of the tile after the next and the
+// values of the next are decoded into the buffers that the first half was the last to
+// read, behind the tile's one barrier.
+template <int D, int NR, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attention_wide_kernel(
     const AttentionArgs a, int few_rows, int tiles) {
-  using S = Wide<D>;
+  using S = Wide<D, NR, WAVES>;
   constexpr int LT = S::kLanes, KS = D / 16, CT = D / 32, L = S::kLoads;
+  constexpr int kThreads = S::kThreads;
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];   // [2] keys, [2] values
   __shared__ int lds_have[4][S::kTile / 16];              // whether a piece has a block
+  uint8_t *const lds_v = lds + 2 * S::kKeys;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, h = lane >> 5;
@@ -80,41 +85,44 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void kv_attention_wide_
   const int rows = req.nq * a.group, rt = index - first_tile(b);
   if (rows <= few_rows || rt < 0 || rt >= req.row_tiles) return;
 
-  // The lane's row, its queries as the right operand, what it sees.  A negative scale
-  // goes into the queries' signs, so that the largest score is the largest product.
-  const int row0 = rt * S::kRows, r = row0 + wave * S::kWaveRows + col;
-  const int i = r / a.group, qh = head * a.group + (r - i * a.group);
-  const bool real = r < rows;
-  u32x4 qf[KS];
+  // The lane's rows, one of each 32; their queries as the right operand, and what they
+  // see.  A negative scale goes into the queries' signs, so that the largest score is the
+  // largest product.
+  const int row0 = rt * S::kRows, w0 = row0 + wave * S::kWaveRows;
+  u32x4 qf[NR][KS];
+  int lo[NR], hi[NR];
   const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
 #pragma unroll
-  for (int k = 0; k < KS; ++k) {
-    qf[k] = u32x4{0, 0, 0, 0};
-    if (real) {
-      qf[k] = *reinterpret_cast<const u32x4 *>(a.q + (req.start + i) * a.q_ts + qh * a.q_hs +
-                                               16 * k + 8 * h);
-      qf[k] ^= flip;
+  for (int n = 0; n < NR; ++n) {
+    const int r = w0 + 32 * n + col, i = r / a.group, qh = head * a.group + (r - i * a.group);
+    const int pos = req.len - req.nq + i;
+    hi[n] = a.causal ? min(pos, req.len - 1) : req.len - 1;
+    lo[n] = a.window ? pos - a.window + 1 : 0;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      qf[n][k] = u32x4{0, 0, 0, 0};
+      if (r < rows) {
+        qf[n][k] = *reinterpret_cast<const u32x4 *>(a.q + (req.start + i) * a.q_ts +
+                                                    qh * a.q_hs + 16 * k + 8 * h);
+        qf[n][k] ^= flip;
+      }
     }
   }
   // (At scale 0 a masked -infinity has to stay one.)
   const float c = fabsf(a.scale_log2) < 0x1p-126f ? 0x1p-126f : fabsf(a.scale_log2);
-  const int pos = req.len - req.nq + i;
-  const int hi = a.causal ? min(pos, req.len - 1) : req.len - 1;
-  const int lo = a.window ? pos - a.window + 1 : 0;
-  // What the wave's rows see: all of them from all_lo to all_hi, none outside any_lo to
-  // any_hi; the workgroup's tiles.
+  // What all of the wave's rows see: all_lo to all_hi; the workgroup's tiles.
   auto position = [&](int row) { return req.len - req.nq + min(row, rows - 1) / a.group; };
-  const int w0 = row0 + wave * S::kWaveRows;
   const int p0 = position(w0), p1 = position(w0 + S::kWaveRows - 1);
-  const int all_hi = a.causal ? p0 : req.len - 1, any_hi = a.causal ? p1 : req.len - 1;
-  const int all_lo = a.window ? p1 - a.window + 1 : 0, any_lo = a.window ? p0 - a.window + 1 : 0;
+  const int all_hi = a.causal ? p0 : req.len - 1, all_lo = a.window ? p1 - a.window + 1 : 0;
   const int g_hi = a.causal ? position(row0 + S::kRows - 1) : req.len - 1;
   const int g_lo = a.window ? max(position(row0) - a.window + 1, 0) : 0;
   const int tile0 = g_lo / S::kTile, end = g_hi < 0 ? 0 : g_hi / S::kTile + 1;
 
   const int32_t *table = a.tables + (int64_t)b * a.width;
   // The thread's blocks of a tile: number n = tid + 256 l, block n % LT of token n / LT.
-  // Scale bytes of both come with the keys; the values follow a step later.
+  // (Where a tile has fewer than 256, two threads do the same.)  Scale bytes of both
+  // come with the keys; the values follow a tile later.
+  const int first_n = S::kBlocks < kThreads ? tid % S::kBlocks : tid;
   u32x4 kc[L], vc[L];
   uint32_t ks[L], vs[L], vs_next[L];
   int64_t at[L];
@@ -122,15 +130,16 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void kv_attention_wide_
   auto look_up = [&](int tile) {
 #pragma unroll
     for (int l = 0; l < L; ++l) {
-      const int t = tile * S::kTile + (tid + kThreads * l) / LT;
+      // (By pieces of 16 tokens, so that all of a piece find the same.)
+      const int t = tile * S::kTile + (first_n + kThreads * l) / (16 * LT) * 16;
       id[l] = -1;
-      if (tid + kThreads * l < S::kBlocks && t < req.len) id[l] = table[t >> a.page_shift];
+      if (t < req.len) id[l] = table[t >> a.page_shift];
     }
   };
   auto fetch_keys = [&](int tile) {
 #pragma unroll
     for (int l = 0; l < L; ++l) {
-      const int n = tid + kThreads * l, t = tile * S::kTile + n / LT;
+      const int n = first_n + kThreads * l, t = tile * S::kTile + n / LT;
       ok[l] = (uint32_t)id[l] < (uint32_t)a.blocks;
       const int64_t row =
           (((int64_t)(ok[l] ? id[l] : 0) * a.heads + head) << a.page_shift) + (t & (a.page - 1));
@@ -147,58 +156,64 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void kv_attention_wide_
       vs[l] = vs_next[l];
     }
   };
-  // A block that is NaN (a value byte that bf16 does not hold) makes its token's scores
-  // NaN; the values in LDS are finite, so that a masked P gives 0.
-  auto decode_keys = [&](int tile) {
-    uint8_t *keys = lds + (tile & 1) * S::kPart;
-#pragma unroll
-    for (int l = 0; l < L; ++l) {
-      const int n = tid + kThreads * l, token = n / LT, block = n % LT;
-      if (S::kBlocks % kThreads == 0 || n < S::kBlocks) {
-        if (n % (16 * LT) == 0) lds_have[tile & 3][token / 16] = ok[l];
-        const bool nan = ks[l] == 0xFFu || vs_next[l] >= 0xFDu;
-        const float sk = scale_operand(ks[l]);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          u32x4 x = decode_bf16(kc[l][w], sk);
-          if (w == 0 && nan) x[0] = 0x7FC07FC0u;
-          *reinterpret_cast<u32x4 *>(keys + S::key(token, 4 * block + w)) = x;
-        }
-      }
+  // Word w of the keys' or values' blocks to LDS.  A block that is NaN (a value byte
+  // that bf16 does not hold) makes its token's scores NaN; the values in LDS are finite,
+  // so that a masked P gives 0.
+  auto decode_key = [&](int buf, int tile, int l, int w) {
+    const int n = first_n + kThreads * l, token = n / LT, block = n % LT;
+    u32x4 x = decode_bf16(kc[l][w], scale_operand(ks[l]));
+    if (w == 0) {
+      if (ks[l] == 0xFFu || vs_next[l] >= 0xFDu) x[0] = 0x7FC07FC0u;
+      lds_have[tile & 3][token / 16] = ok[l];             // (the same from all of a piece)
     }
+    *reinterpret_cast<u32x4 *>(lds + buf * S::kKeys + token * S::kKeyPitch + 64 * block + 16 * w) =
+        x;
   };
-  auto decode_values = [&](int tile) {
-    uint8_t *vals = lds + (2 + (tile & 1)) * S::kPart;
+  auto decode_value = [&](int buf, int l, int w) {
+    const int n = first_n + kThreads * l, token = n / LT, block = n % LT;
+    *reinterpret_cast<u32x4 *>(lds_v + buf * S::kValues + token * S::kValuePitch + 64 * block +
+                               16 * w) =
+        decode_bf16(vc[l][w], scale_operand(vs[l] < 0xFDu ? vs[l] : 0u));
+  };
+  auto decode_keys = [&](int buf, int tile) {
 #pragma unroll
-    for (int l = 0; l < L; ++l) {
-      const int n = tid + kThreads * l, token = n / LT, block = n % LT;
-      if (S::kBlocks % kThreads == 0 || n < S::kBlocks) {
-        const float sv = scale_operand(vs[l] < 0xFDu ? vs[l] : 0u);
+    for (int x = 0; x < 4 * L; ++x) decode_key(buf, tile, x / 4, x % 4);
+  };
+  auto decode_values = [&](int buf) {
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
-          *reinterpret_cast<u32x4 *>(vals + S::value(token, 2 * block + w / 2) + 16 * (w % 2)) =
-              decode_bf16(vc[l][w], sv);
-      }
-    }
+    for (int x = 0; x < 4 * L; ++x) decode_value(buf, x / 4, x % 4);
   };
 
-  v16f o[CT];
+  v16f o[NR][CT], s[2][NR];
+  u32x2 pf[2][NR][4];                                     // P of a half, 4 tokens each
+  float m[NR], sum[NR];                                   // m: in units of log2
 #pragma unroll
-  for (int t = 0; t < CT; ++t) o[t] = v16f{};
-  float m = neg_inf(), sum = 0.0f;                        // m: in units of log2
-  // Whether some row of the wave sees something of a tile.
-  auto seen = [&](int tile) {
-    return tile < end && tile * S::kTile <= any_hi && (tile + 1) * S::kTile > any_lo;
+  for (int n = 0; n < NR; ++n) {
+#pragma unroll
+    for (int t = 0; t < CT; ++t) o[n][t] = v16f{};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) pf[1][n][q] = u32x2{0, 0};
+    m[n] = neg_inf();
+    sum[n] = 0.0f;
+  }
+  const int l16 = lane & 15, ch16 = lane >> 4 & 1;
+  // Operand k of a half's keys; operand (u, t) of its values (16 tokens u, 32 channels
+  // t; tokens 4 h + 0..3 and 8 further: the order in which P holds them).
+  auto key_frag = [&](int buf, int t, int k) {
+    return *reinterpret_cast<const u32x4 *>(lds + buf * S::kKeys + col * S::kKeyPitch + 16 * h +
+                                            32 * t * S::kKeyPitch + 32 * k);
   };
-  v16f s[2];
-  // Half t of a tile's scores.
-  auto score = [&](int tile, int t) {
-    const uint8_t *keys = lds + (tile & 1) * S::kPart;
-    s[t] = v16f{};
-#pragma unroll
-    for (int k = 0; k < KS; ++k)
-      s[t] = mma32(*reinterpret_cast<const u32x4 *>(keys + S::key(32 * t + col, 2 * k + h)), qf[k],
-                   s[t]);
+  auto value_frag = [&](int buf, int t, int f) {
+    const uint8_t *src = lds_v + buf * S::kValues + (4 * h + (l16 >> 2)) * S::kValuePitch +
+                         32 * ch16 + 8 * (l16 & 3) +
+                         (32 * t + 16 * (f / CT)) * S::kValuePitch + 64 * (f % CT);
+    const u32x2 v0 = read_transposed(src);
+    const u32x2 v1 = read_transposed(src + 8 * S::kValuePitch);
+    return u32x4{v0[0], v0[1], v1[0], v1[1]};
+  };
+  auto weights = [&](const u32x2 (&p)[4], int f) {
+    const int u = f / CT;
+    return u32x4{p[2 * u][0], p[2 * u][1], p[2 * u + 1][0], p[2 * u + 1][1]};
   };
 
   if (tile0 < end) {
@@ -206,135 +221,179 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void kv_attention_wide_
     fetch_keys(tile0);
     fetch_values();
     look_up(tile0 + 1);
-    decode_keys(tile0);
+    decode_keys(0, tile0);
     fetch_keys(tile0 + 1);
     look_up(tile0 + 2);
-    decode_values(tile0);
+    decode_values(0);
+    decode_values(1);                                     // (read with P = 0: finite)
     fetch_values();
-    decode_keys(tile0 + 1);
+    decode_keys(1, tile0 + 1);
     fetch_keys(tile0 + 2);
     look_up(tile0 + 3);
     __syncthreads();
-    score(tile0, 0);
-    score(tile0, 1);
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      s[0][n] = v16f{};
+#pragma unroll
+      for (int k = 0; k < KS; ++k) s[0][n] = mma32(key_frag(0, 0, k), qf[n][k], s[0][n]);
+    }
   }
-  for (int tile = tile0; tile < end; ++tile) {
-    const int t0 = tile * S::kTile;
-    const bool now = seen(tile);
-    if (now) {
-      int have[4];
+  // Half T of a tile.
+  auto step = [&](int tile, auto half) {
+    constexpr int T = decltype(half)::value, N = 1 - T;
+    const int buf = (tile - tile0) & 1;
+    const int keys = buf ^ T;                             // of S_(j+1), half N
+    const int vals = buf ^ N;                             // of P_(j-1), half N
+    const int t0 = tile * S::kTile + 32 * T;
+    constexpr int kAhead = 2;
+    u32x4 kf[KS], vf[KS];
 #pragma unroll
-      for (int p = 0; p < 4; ++p) have[p] = lds_have[tile & 3][p];
-      const bool whole = (have[0] & have[1] & have[2] & have[3]) && t0 >= all_lo &&
-                         t0 + S::kTile - 1 <= all_hi;
-      if (!__builtin_amdgcn_readfirstlane(whole)) {
-        asm volatile("");                                 // (a branch, not selects)
+    for (int k = 0; k < kAhead; ++k) {
+      kf[k] = key_frag(keys, N, k);
+      vf[k] = value_frag(vals, N, k);
+    }
+    const int have0 = lds_have[tile & 3][2 * T], have1 = lds_have[tile & 3][2 * T + 1];
+    const bool whole = (have0 & have1) && t0 >= all_lo && t0 + 31 <= all_hi;
+    if (!__builtin_amdgcn_readfirstlane(whole)) {
+      asm volatile("");                                   // (a branch, not selects)
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+      for (int n = 0; n < NR; ++n)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int tok = t0 + 32 * t + 8 * (e / 4) + 4 * h + e % 4;
-            const bool see = tok >= lo && tok <= hi && have[2 * t + e / 8];
-            s[t][e] = see ? s[t][e] : neg_inf();
+        for (int e = 0; e < 16; ++e) {
+          const int tok = t0 + 8 * (e / 4) + 4 * h + e % 4;
+          const bool see = tok >= lo[n] && tok <= hi[n] && (e < 8 ? have0 : have1);
+          s[T][n][e] = see ? s[T][n][e] : neg_inf();
+        }
+    }
+    float top[NR];
+    bool grows = false;
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      float x = s[T][n][0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) x = fmaxf(x, s[T][n][e]);
+      const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x),
+                                                         false, false);
+      top[n] = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * c;
+      grows |= top[n] > m[n] + 8.0f;
+    }
+    // The reference follows the maximum only where P would pass 2^8, to a whole power
+    // of two: P_(j-1), still to be multiplied, is scaled exactly.
+    if (__any(grows)) {
+      asm volatile("");
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        const float up = fmaxf(ceilf(top[n]), m[n]);
+        const float f = exp2_hw(m[n] - (up == neg_inf() ? 0.0f : up));
+        sum[n] *= f;
+#pragma unroll
+        for (int t = 0; t < CT; ++t) o[n][t] *= f;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const uint32_t p = pf[N][n][q][x];
+            const bf16x2 y = {(__bf16)(__uint_as_float(p << 16) * f),
+                              (__bf16)(__uint_as_float(p & 0xFFFF0000u) * f)};
+            pf[N][n][q][x] = __builtin_bit_cast(uint32_t, y);
           }
-      }
-      float top = s[0][0];
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][e]);
-      const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top),
-                                                         __float_as_uint(top), false, false);
-      top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * c;
-      // The reference follows the maximum only where P would pass 2^8.
-      if (__any(top > m + 8.0f)) {
-        asm volatile("");
-        const float up = fmaxf(top, m);
-        const float f = exp2_hw(m - (up == neg_inf() ? 0.0f : up));
-        sum *= f;
-#pragma unroll
-        for (int t = 0; t < CT; ++t) o[t] *= f;
-        m = up;
+        m[n] = up;
       }
     }
-    u32x2 pf[2][4];
-    const float ref = m == neg_inf() ? 0.0f : m;
-    auto weigh = [&](int t, int q) {
-      float e[4];
+    float ref[NR], e[NR][16];
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        e[x] = exp2_hw(__builtin_fmaf(s[t][4 * q + x], c, -ref));
-        sum += e[x];
+    for (int n = 0; n < NR; ++n) {
+      ref[n] = m[n] == neg_inf() ? 0.0f : m[n];
+      s[N][n] = v16f{};
+    }
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      if (k + kAhead < KS) {
+        kf[k + kAhead] = key_frag(keys, N, k + kAhead);
+        vf[k + kAhead] = value_frag(vals, N, k + kAhead);
       }
-      const bf16x4 y = {(__bf16)e[0], (__bf16)e[1], (__bf16)e[2], (__bf16)e[3]};
-      pf[t][q] = __builtin_bit_cast(u32x2, y);
-    };
-    if (now) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) weigh(0, q);
-      score(tile + 1, 0);
+      for (int n = 0; n < NR; ++n) {
+        s[N][n] = mma32(kf[k], qf[n][k], s[N][n]);
+        o[n][k % CT] = mma32(vf[k], weights(pf[N][n], k), o[n][k % CT]);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) weigh(1, q);
-      score(tile + 1, 1);
-      const uint8_t *vals = lds + (2 + (tile & 1)) * S::kPart;
-      // Tokens 16 u + 4 h + 0..3 and + 8 of it: the order in which P holds them.
-      const int l16 = lane & 15, half = lane >> 4 & 1;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const u32x4 p = {pf[u / 2][u % 2 * 2][0], pf[u / 2][u % 2 * 2][1],
-                         pf[u / 2][u % 2 * 2 + 1][0], pf[u / 2][u % 2 * 2 + 1][1]};
-        const int token = 16 * u + 4 * h + (l16 >> 2);
-#pragma unroll
-        for (int t = 0; t < CT; ++t) {
-          const u32x2 v0 = read_transposed(vals + S::value(token, 2 * t + half) + (l16 & 3) * 8);
-          const u32x2 v1 =
-              read_transposed(vals + S::value(token + 8, 2 * t + half) + (l16 & 3) * 8);
-          o[t] = mma32(u32x4{v0[0], v0[1], v1[0], v1[1]}, p, o[t]);
+        for (int x = k * 16 / KS; x < (k + 1) * 16 / KS; ++x) {
+          e[n][x] = exp2_hw(__builtin_fmaf(s[T][n][x], c, -ref[n]));
+          if (x % 4 == 3) {
+            const bf16x4 y = {(__bf16)e[n][x - 3], (__bf16)e[n][x - 2], (__bf16)e[n][x - 1],
+                              (__bf16)e[n][x]};
+            u32x2 &p = pf[T][n][x / 4];
+            p = __builtin_bit_cast(u32x2, y);
+            sum[n] += (e[n][x - 3] + e[n][x - 2]) + (e[n][x - 1] + e[n][x]);
+            // (Not to be moved behind the products.)
+            asm volatile("" : "+v"(p[0]), "+v"(p[1]), "+v"(sum[n]));
+          }
         }
       }
-    } else {
-      score(tile + 1, 0);
-      score(tile + 1, 1);
+      if constexpr (T == 1) {
+        // The next codes to LDS, keys first; then the loads that take their registers.
+#pragma unroll
+        for (int x = k * 8 * L / KS; x < (k + 1) * 8 * L / KS; ++x) {
+          if (x < 4 * L) decode_key(buf, tile + 2, x / 4, x % 4);
+          else decode_value(buf ^ 1, x / 4 - L, x % 4);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
-    // (Tiles past the end are decoded and scored too: from places that exist, not used.)
-    decode_values(tile + 1);
-    fetch_values();
-    decode_keys(tile + 2);
-    fetch_keys(tile + 3);
-    look_up(tile + 4);
+    if constexpr (T == 1) {
+      fetch_values();
+      fetch_keys(tile + 3);
+      look_up(tile + 4);
+    }
+  };
+  // (Tiles past the end are decoded and scored too: from places that exist, not used.)
+  for (int tile = tile0; tile < end; ++tile) {
+    step(tile, std::integral_constant<int, 0>{});
     __syncthreads();
+    step(tile, std::integral_constant<int, 1>{});
+  }
+  if (tile0 < end) {
+    const int buf = (end - 1 - tile0) & 1;
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+      for (int f = 0; f < KS; ++f)
+        o[n][f % CT] = mma32(value_frag(buf, 1, f), weights(pf[1][n], f), o[n][f % CT]);
   }
 
-  const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum),
-                                                     false, false);
-  sum = __uint_as_float(both[0]) + __uint_as_float(both[1]);
-  if (!real) return;
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  uint16_t *out = a.out + (req.start + i) * a.o_ts + qh * a.o_hs;
 #pragma unroll
-  for (int t = 0; t < CT; ++t)
+  for (int n = 0; n < NR; ++n) {
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum[n]),
+                                                       __float_as_uint(sum[n]), false, false);
+    const float l = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+    const int r = w0 + 32 * n + col, i = r / a.group, qh = head * a.group + (r - i * a.group);
+    if (r >= rows) continue;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    uint16_t *out = a.out + (req.start + i) * a.o_ts + qh * a.o_hs;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const bf16x4 y = {(__bf16)(o[t][4 * q] * inv), (__bf16)(o[t][4 * q + 1] * inv),
-                        (__bf16)(o[t][4 * q + 2] * inv), (__bf16)(o[t][4 * q + 3] * inv)};
-      *reinterpret_cast<u32x2 *>(out + 32 * t + 8 * q + 4 * h) = __builtin_bit_cast(u32x2, y);
-    }
-  if (a.lse && h == 0)
-    a.lse[(int64_t)(req.start + i) * a.Hq + qh] =
-        sum == 0.0f ? neg_inf() : (m + __builtin_amdgcn_logf(sum)) * kLn2;
+    for (int t = 0; t < CT; ++t)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const v16f &x = o[n][t];
+        const bf16x4 y = {(__bf16)(x[4 * q] * inv), (__bf16)(x[4 * q + 1] * inv),
+                          (__bf16)(x[4 * q + 2] * inv), (__bf16)(x[4 * q + 3] * inv)};
+        *reinterpret_cast<u32x2 *>(out + 32 * t + 8 * q + 4 * h) = __builtin_bit_cast(u32x2, y);
+      }
+    if (a.lse && h == 0)
+      a.lse[(int64_t)(req.start + i) * a.Hq + qh] =
+          l == 0.0f ? neg_inf() : (m[n] + __builtin_amdgcn_logf(l)) * kLn2;
+  }
 }
 
-std::atomic<bool> g_lds_limit[3][kMaxDevices];
-
-template <int D>
+template <int D, int NR, int WAVES>
 hipError_t launch(const AttentionArgs &a, int few_rows, hipStream_t stream) {
-  using S = Wide<D>;
-  const hipError_t e = set_lds_limit(g_lds_limit[D == 64 ? 0 : (D == 128 ? 1 : 2)],
-                                     (const void *)kv_attention_wide_kernel<D>, S::kLds);
+  using S = Wide<D, NR, WAVES>;
+  static std::atomic<bool> limit[kMaxDevices];
+  const auto kernel = kv_attention_wide_kernel<D, NR, WAVES>;
+  const hipError_t e = set_lds_limit(limit, (const void *)kernel, S::kLds);
   if (e != hipSuccess) return e;
   const int64_t tiles = (int64_t)a.T * a.group / S::kRows + a.B;
-  kv_attention_wide_kernel<D><<<(unsigned)(tiles * a.heads), kThreads, S::kLds, stream>>>(
-      a, few_rows, (int)tiles);
+  kernel<<<(unsigned)(tiles * a.heads), S::kThreads, S::kLds, stream>>>(a, few_rows, (int)tiles);
   return hipGetLastError();
 }
 
@@ -342,9 +401,9 @@ hipError_t launch(const AttentionArgs &a, int few_rows, hipStream_t stream) {
 
 hipError_t launch_kv_attention_wide(const AttentionArgs &a, int64_t D, int few_rows,
                                     hipStream_t stream) {
-  if (D == 64) return launch<64>(a, few_rows, stream);
-  if (D == 128) return launch<128>(a, few_rows, stream);
-  return launch<256>(a, few_rows, stream);
+  if (D == 64) return launch<64, 1, 4>(a, few_rows, stream);
+  if (D == 128) return launch<128, 1, 4>(a, few_rows, stream);
+  return launch<256, 1, 4>(a, few_rows, stream);
 }
 
 }  // namespace rfq
