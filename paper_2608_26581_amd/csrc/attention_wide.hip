@@ -23,10 +23,24 @@ namespace rfq {
 namespace {
 
 typedef float v16f __attribute__((ext_vector_type(16)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+// Products that an operand is read from LDS before it is used.
+constexpr int kReadAhead = 3;
 
 __device__ __forceinline__ v16f mma32(const u32x4 &a, const u32x4 &b, const v16f &c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
                                                  __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// The two codes of byte w (a constant) to bf16 times their scale.
+__device__ __forceinline__ uint32_t decode_pair(uint32_t c, float s, int w) {
+  bf16x2 r;
+  if (w == 0) r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0);
+  else if (w == 1) r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1);
+  else if (w == 2) r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2);
+  else r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3);
+  return __builtin_bit_cast(uint32_t, r);
 }
 
 template <int D, int NR, int WAVES>
@@ -36,14 +50,16 @@ struct Wide {
   static constexpr int kLanes = D / 32;                   // 32-channel blocks of a token
   static constexpr int kBlocks = kTile * kLanes;          // of a tile
   static constexpr int kLoads = (kBlocks + kThreads - 1) / kThreads;
-  // Rows in LDS are padded so that what 16 lanes read or write at once lies in
-  // different banks (at 128 channels; nearly so at 64 and 256): 16 bytes of 16 tokens (the
-  // keys' operand), 64 bytes of 4 neighbouring tokens (what transposing reads of the
-  // values take), and 16 bytes of every block of some tokens when either is written.  All
-  // addresses are then one of four registers and a constant.
-  static constexpr int kKeyPitch = 2 * D + 16, kValuePitch = 2 * D + 80;
-  static constexpr int kKeys = kTile * kKeyPitch, kValues = kTile * kValuePitch;
-  static constexpr int kLds = 2 * (kKeys + kValues);      // two tiles
+  // In LDS the keys are rows of channels, the values rows of tokens (transposed while
+  // they are decoded: a transposing read takes twice the LDS time of a plain one), with
+  // the channel of row r r % (D / 8) * 8 + r / (D / 8) and the tokens in the order in which P
+  // holds them.  Rows are padded by 16 bytes so that what 16 lanes read or write at once
+  // lies in different banks; all addresses are one of a few registers and a constant.
+  static constexpr int kOctets = D / 8;
+  static constexpr int kKeyPitch = 2 * D + 16, kValuePitch = 2 * kTile + 16;
+  static constexpr int kKeys = kTile * kKeyPitch, kValues = D * kValuePitch;
+  static constexpr int kScales = kBlocks;                 // the values' scale bytes [block][token]
+  static constexpr int kLds = 2 * (kKeys + kValues + kScales);    // two tiles
 };
 
 // Requests with more than few_rows rows (the others are attention.hip's).  The row
@@ -63,8 +79,8 @@ __global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attentio
   constexpr int LT = S::kLanes, KS = D / 16, CT = D / 32, L = S::kLoads;
   constexpr int kThreads = S::kThreads;
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];   // [2] keys, [2] values
-  __shared__ int lds_have[4][S::kTile / 16];              // whether a piece has a block
-  uint8_t *const lds_v = lds + 2 * S::kKeys;
+  __shared__ alignas(16) int lds_have[4][S::kTile / 16];              // whether a piece has a block
+  uint8_t *const lds_v = lds + 2 * S::kKeys, *const lds_s = lds_v + 2 * S::kValues;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, h = lane >> 5;
@@ -119,18 +135,20 @@ __global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attentio
   const int tile0 = g_lo / S::kTile, end = g_hi < 0 ? 0 : g_hi / S::kTile + 1;
 
   const int32_t *table = a.tables + (int64_t)b * a.width;
-  // The thread's blocks of a tile: number n = tid + 256 l, block n % LT of token n / LT.
-  // (Where a tile has fewer than 256, two threads do the same.)  Scale bytes of both
-  // come with the keys; the values follow a tile later.
+  // The thread's part of a tile.  Keys: block n % LT of token n / LT, n = tid + 256 l.
+  // Values, a tile later: 8 channels n % kOctets of the 4 tokens n / kOctets, which are in
+  // the same piece of 16 tokens as its keys.  (Where a tile has fewer than 256 of them, two
+  // threads do the same.)
   const int first_n = S::kBlocks < kThreads ? tid % S::kBlocks : tid;
-  u32x4 kc[L], vc[L];
-  uint32_t ks[L], vs[L], vs_next[L];
-  int64_t at[L];
+  u32x4 kc[L], vc[L];                                     // vc: a token's 8 codes each
+  uint32_t ks[L], vs[L];
+  const uint32_t *v_from[L];
+  float sv[L][4];
   int id[L], ok[L];
   auto look_up = [&](int tile) {
 #pragma unroll
     for (int l = 0; l < L; ++l) {
-      // (By pieces of 16 tokens, so that all of a piece find the same.)
+      // (By pieces, so that all of a piece find the same.)
       const int t = tile * S::kTile + (first_n + kThreads * l) / (16 * LT) * 16;
       id[l] = -1;
       if (t < req.len) id[l] = table[t >> a.page_shift];
@@ -139,41 +157,57 @@ __global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attentio
   auto fetch_keys = [&](int tile) {
 #pragma unroll
     for (int l = 0; l < L; ++l) {
-      const int n = first_n + kThreads * l, t = tile * S::kTile + n / LT;
+      const int n = first_n + kThreads * l, token = n / LT, quad = n / S::kOctets * 4;
       ok[l] = (uint32_t)id[l] < (uint32_t)a.blocks;
-      const int64_t row =
-          (((int64_t)(ok[l] ? id[l] : 0) * a.heads + head) << a.page_shift) + (t & (a.page - 1));
-      at[l] = row * LT + n % LT;
-      kc[l] = reinterpret_cast<const u32x4 *>(a.k_codes)[at[l]];
-      ks[l] = a.k_scales[at[l]];
-      vs_next[l] = a.v_scales[at[l]];
+      const int64_t row = (((int64_t)(ok[l] ? id[l] : 0) * a.heads + head) << a.page_shift) +
+                          ((tile * S::kTile + (token & ~15)) & (a.page - 1));
+      const int64_t at = (row + (token & 15)) * LT + n % LT;
+      kc[l] = reinterpret_cast<const u32x4 *>(a.k_codes)[at];
+      ks[l] = a.k_scales[at];
+      vs[l] = a.v_scales[at];
+      v_from[l] = reinterpret_cast<const uint32_t *>(a.v_codes) +
+                  (row + (quad & 15)) * S::kOctets + n % S::kOctets;
     }
   };
   auto fetch_values = [&] {
 #pragma unroll
-    for (int l = 0; l < L; ++l) {
-      vc[l] = reinterpret_cast<const u32x4 *>(a.v_codes)[at[l]];
-      vs[l] = vs_next[l];
-    }
+    for (int l = 0; l < L; ++l)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) vc[l][i] = v_from[l][i * S::kOctets];
   };
-  // Word w of the keys' or values' blocks to LDS.  A block that is NaN (a value byte
+  // Part w of the thread's keys and values to LDS.  A block that is NaN (a value byte
   // that bf16 does not hold) makes its token's scores NaN; the values in LDS are finite,
   // so that a masked P gives 0.
   auto decode_key = [&](int buf, int tile, int l, int w) {
     const int n = first_n + kThreads * l, token = n / LT, block = n % LT;
     u32x4 x = decode_bf16(kc[l][w], scale_operand(ks[l]));
     if (w == 0) {
-      if (ks[l] == 0xFFu || vs_next[l] >= 0xFDu) x[0] = 0x7FC07FC0u;
+      if (ks[l] == 0xFFu || vs[l] >= 0xFDu) x[0] = 0x7FC07FC0u;
       lds_have[tile & 3][token / 16] = ok[l];             // (the same from all of a piece)
+      lds_s[buf * S::kScales + block * S::kTile + token] = vs[l] < 0xFDu ? (uint8_t)vs[l] : 0;
     }
     *reinterpret_cast<u32x4 *>(lds + buf * S::kKeys + token * S::kKeyPitch + 64 * block + 16 * w) =
         x;
   };
   auto decode_value = [&](int buf, int l, int w) {
-    const int n = first_n + kThreads * l, token = n / LT, block = n % LT;
-    *reinterpret_cast<u32x4 *>(lds_v + buf * S::kValues + token * S::kValuePitch + 64 * block +
-                               16 * w) =
-        decode_bf16(vc[l][w], scale_operand(vs[l] < 0xFDu ? vs[l] : 0u));
+    const int n = first_n + kThreads * l, octet = n % S::kOctets, quad = n / S::kOctets;
+    if (w == 0) {
+      const uint32_t scales = *reinterpret_cast<const uint32_t *>(
+          lds_s + buf * S::kScales + octet / 4 * S::kTile + 4 * quad);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sv[l][i] = scale_operand(c_byte(scales, i));
+    }
+    uint32_t x[4];                                        // channels 2 w and 2 w + 1 of a token
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = decode_pair(vc[l][i], sv[l][i], w);
+    // Four tokens of a channel; quads of 16 tokens in the order 0, 2, 1, 3.
+    uint8_t *to = lds_v + buf * S::kValues + (2 * w * S::kOctets + octet) * S::kValuePitch +
+                  (quad >> 2) * 32 + (quad & 1) * 16 + (quad >> 1 & 1) * 8;
+    *reinterpret_cast<u32x2 *>(to) = u32x2{__builtin_amdgcn_perm(x[1], x[0], 0x05040100u),
+                                           __builtin_amdgcn_perm(x[3], x[2], 0x05040100u)};
+    *reinterpret_cast<u32x2 *>(to + S::kOctets * S::kValuePitch) =
+        u32x2{__builtin_amdgcn_perm(x[1], x[0], 0x07060302u),
+              __builtin_amdgcn_perm(x[3], x[2], 0x07060302u)};
   };
   auto decode_keys = [&](int buf, int tile) {
 #pragma unroll
@@ -196,20 +230,15 @@ __global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attentio
     m[n] = neg_inf();
     sum[n] = 0.0f;
   }
-  const int l16 = lane & 15, ch16 = lane >> 4 & 1;
-  // Operand k of a half's keys; operand (u, t) of its values (16 tokens u, 32 channels
-  // t; tokens 4 h + 0..3 and 8 further: the order in which P holds them).
+  // Operand k of a half's keys; operand (u, t) of its values (16 tokens u, 32 rows t).
   auto key_frag = [&](int buf, int t, int k) {
     return *reinterpret_cast<const u32x4 *>(lds + buf * S::kKeys + col * S::kKeyPitch + 16 * h +
                                             32 * t * S::kKeyPitch + 32 * k);
   };
   auto value_frag = [&](int buf, int t, int f) {
-    const uint8_t *src = lds_v + buf * S::kValues + (4 * h + (l16 >> 2)) * S::kValuePitch +
-                         32 * ch16 + 8 * (l16 & 3) +
-                         (32 * t + 16 * (f / CT)) * S::kValuePitch + 64 * (f % CT);
-    const u32x2 v0 = read_transposed(src);
-    const u32x2 v1 = read_transposed(src + 8 * S::kValuePitch);
-    return u32x4{v0[0], v0[1], v1[0], v1[1]};
+    return *reinterpret_cast<const u32x4 *>(lds_v + buf * S::kValues + col * S::kValuePitch +
+                                            16 * h + f % CT * 32 * S::kValuePitch +
+                                            (2 * t + f / CT) * 32);
   };
   auto weights = [&](const u32x2 (&p)[4], int f) {
     const int u = f / CT;
@@ -224,8 +253,10 @@ __global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attentio
     decode_keys(0, tile0);
     fetch_keys(tile0 + 1);
     look_up(tile0 + 2);
+    __syncthreads();                                      // (the values' scales)
     decode_values(0);
-    decode_values(1);                                     // (read with P = 0: finite)
+    for (int i = tid * 16; i < S::kValues; i += kThreads * 16)       // (read with P = 0)
+      *reinterpret_cast<u32x4 *>(lds_v + S::kValues + i) = u32x4{0, 0, 0, 0};
     fetch_values();
     decode_keys(1, tile0 + 1);
     fetch_keys(tile0 + 2);
@@ -238,6 +269,10 @@ __global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attentio
       for (int k = 0; k < KS; ++k) s[0][n] = mma32(key_frag(0, 0, k), qf[n][k], s[0][n]);
     }
   }
+  // Which pieces of a tile have a block: read a step before it is needed.
+  auto find = [&](int tile) { return *reinterpret_cast<const i32x4 *>(lds_have[tile & 3]); };
+  i32x4 have = {0, 0, 0, 0};
+  if (tile0 < end) have = find(tile0);
   // Half T of a tile.
   auto step = [&](int tile, auto half) {
     constexpr int T = decltype(half)::value, N = 1 - T;
@@ -245,14 +280,14 @@ __global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attentio
     const int keys = buf ^ T;                             // of S_(j+1), half N
     const int vals = buf ^ N;                             // of P_(j-1), half N
     const int t0 = tile * S::kTile + 32 * T;
-    constexpr int kAhead = 2;
+    constexpr int kAhead = kReadAhead < KS ? kReadAhead : KS;
     u32x4 kf[KS], vf[KS];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       kf[k] = key_frag(keys, N, k);
       vf[k] = value_frag(vals, N, k);
     }
-    const int have0 = lds_have[tile & 3][2 * T], have1 = lds_have[tile & 3][2 * T + 1];
+    const int have0 = have[2 * T], have1 = have[2 * T + 1];
     const bool whole = (have0 & have1) && t0 >= all_lo && t0 + 31 <= all_hi;
     if (!__builtin_amdgcn_readfirstlane(whole)) {
       asm volatile("");                                   // (a branch, not selects)
@@ -331,6 +366,7 @@ __global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attentio
         }
       }
       if constexpr (T == 1) {
+        if (k == 0) have = find(tile + 1);
         // The next codes to LDS, keys first; then the loads that take their registers.
 #pragma unroll
         for (int x = k * 8 * L / KS; x < (k + 1) * 8 * L / KS; ++x) {
@@ -370,15 +406,25 @@ __global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attentio
     if (r >= rows) continue;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     uint16_t *out = a.out + (req.start + i) * a.o_ts + qh * a.o_hs;
+    // Element e of tile t is row 32 t + 8 (e / 4) + 4 h + e % 4: 8 channels in the order of
+    // memory are those whose rows are D / 8 apart.
 #pragma unroll
-    for (int t = 0; t < CT; ++t)
+    for (int g = 0; g < D / 16; ++g) {
+      u32x4 y;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const v16f &x = o[n][t];
-        const bf16x4 y = {(__bf16)(x[4 * q] * inv), (__bf16)(x[4 * q + 1] * inv),
-                          (__bf16)(x[4 * q + 2] * inv), (__bf16)(x[4 * q + 3] * inv)};
-        *reinterpret_cast<u32x2 *>(out + 32 * t + 8 * q + 4 * h) = __builtin_bit_cast(u32x2, y);
+      for (int k = 0; k < 8; k += 2) {
+        float v[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          // Row of the k-th channel of the lane's g-th octet (without 4 h).
+          const int row = (k + x) * S::kOctets + g / 4 * 8 + g % 4;
+          v[x] = o[n][row / 32][row % 32 / 8 * 4 + row % 4] * inv;
+        }
+        const bf16x2 p = {(__bf16)v[0], (__bf16)v[1]};
+        y[k / 2] = __builtin_bit_cast(uint32_t, p);
       }
+      *reinterpret_cast<u32x4 *>(out + 8 * (g / 4 * 8 + 4 * h + g % 4)) = y;
+    }
     if (a.lse && h == 0)
       a.lse[(int64_t)(req.start + i) * a.Hq + qh] =
           l == 0.0f ? neg_inf() : (m[n] + __builtin_amdgcn_logf(l)) * kLn2;
