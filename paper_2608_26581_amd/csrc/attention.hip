@@ -33,6 +33,9 @@ constexpr int kSplitGroups = 512;
 // An item's queries, its first loads and the joining of the waves take about as long
 // as this many tiles.
 constexpr int kItemCost = 4;
+// Workgroups of a launch, and the tokens of a part of the wide kernel's, at least.
+constexpr int64_t kMaxGrid = int64_t(1) << 20;
+constexpr int64_t kLeastPart = 1024;
 
 // ---- the shapes and the requests
 
@@ -577,7 +580,7 @@ hipError_t launch(const AttentionArgs &a, bool split, float *work, hipStream_t s
   } else {
     // At least as many workgroups as there are items, within a launch's limits.
     const int64_t items = (up((int64_t)a.T * a.group, S::kRows) + a.B) * a.heads;
-    grid = (unsigned)(items < (1 << 20) ? items : (1 << 20));
+    grid = (unsigned)(items < kMaxGrid ? items : kMaxGrid);
   }
   kv_attention_kernel<D, NT><<<grid, kThreads, 0, stream>>>(a, p, split);
   hipError_t e = hipGetLastError();
@@ -587,52 +590,71 @@ hipError_t launch(const AttentionArgs &a, bool split, float *work, hipStream_t s
   return hipGetLastError();
 }
 
-// Requests up to this many rows (queries times group) never take the wide kernel.
-constexpr int kFewRows = 64;
-constexpr int64_t kWideTiles = 128;
-
 // No split where every request's tokens are a step or two of a workgroup's waves.
 bool splits(int64_t max_seq) { return max_seq > 256; }
 
-// Whether requests with many rows take the wide kernel: it does not split tokens, so its
-// row tiles alone have to fill the GPU (and fit a launch).
-bool wide_applies(int64_t T, int64_t group, int64_t heads, int64_t B, int64_t max_query) {
-  const int64_t tiles = T * group / 128 * heads;
-  return max_query * group > kFewRows && tiles >= kWideTiles &&
-         tiles + B * heads <= UINT32_MAX / kThreads;
+// What a call launches.  Requests of up to kFewRows rows (queries times group) never take
+// the wide kernel; with one request the wide kernel alone serves it, whatever its rows.
+constexpr int kFewRows = 64;
+struct Plan {
+  bool few, wide;
+  int few_rows;                           // the wide kernel's requests have more
+  int nt;                                 // 16-row fragments of the other kernel
+  int wide_parts;
+  int64_t few_bytes, wide_work;           // workspace of each (0: no split)
+};
+Plan plan_of(int64_t T, int64_t group, int64_t heads, int64_t D, int64_t B, int64_t max_query,
+             int64_t max_seq, int64_t bytes) {
+  Plan p = {};
+  const int64_t items = wide_tiles(T, group, B) * heads;
+  p.wide = max_query * group > kFewRows && items > 0 && items <= kMaxGrid;
+  p.few = !p.wide || B > 1;
+  p.few_rows = p.wide ? (B > 1 ? kFewRows : 0) : INT32_MAX;
+  const int64_t rows = max_query * group;
+  p.nt = row_fragments(p.wide && rows > kFewRows ? kFewRows : rows, D);
+  p.few_bytes = p.few && splits(max_seq) ? partial_bytes(D, p.nt) : 0;
+  p.wide_parts = 1;
+  if (p.wide) {
+    // Two workgroups a CU; a part is at least kLeastPart tokens.
+    const int64_t room = 512 / items;
+    const int64_t most = max_seq / kLeastPart;
+    const int64_t parts = room < most ? room : most;
+    p.wide_parts = (int)(parts < 1 ? 1 : (parts > 32 ? 32 : parts));
+    p.wide_work = wide_bytes(items, p.wide_parts, D);
+  }
+  if (bytes >= 0 && bytes < p.few_bytes + p.wide_work) {
+    p.few_bytes = p.wide_work = 0;
+    p.wide_parts = 1;
+  }
+  return p;
 }
 
 }  // namespace
 
 int64_t kv_attention_workspace(int64_t T, int64_t Hq, int64_t heads, int64_t D, int64_t B,
                                int64_t max_query, int64_t max_seq) {
-  if (!splits(max_seq)) return 0;
-  if (wide_applies(T, Hq / heads, heads, B, max_query)) {
-    if (B == 1) return 0;
-    max_query = kFewRows;
-  }
-  return partial_bytes(D, row_fragments(max_query * (Hq / heads), D));
+  const Plan p = plan_of(T, Hq / heads, heads, D, B, max_query, max_seq, -1);
+  return p.few_bytes + p.wide_work;
 }
 
 hipError_t launch_kv_attention(const AttentionArgs &args, int64_t D, int64_t max_query,
                                int64_t max_seq, float *workspace, int64_t workspace_bytes,
                                hipStream_t stream) {
   AttentionArgs a = args;
-  a.most_rows = INT32_MAX;
-  if (wide_applies(a.T, a.group, a.heads, a.B, max_query)) {
-    a.most_rows = a.B == 1 ? 0 : kFewRows;
-    const hipError_t e = launch_kv_attention_wide(a, D, a.most_rows, stream);
-    if (e != hipSuccess || a.B == 1) return e;
-    max_query = (kFewRows + a.group - 1) / a.group;
+  const Plan p = plan_of(a.T, a.group, a.heads, D, a.B, max_query, max_seq, workspace_bytes);
+  a.most_rows = p.few_rows;
+  if (p.wide) {
+    const hipError_t e = launch_kv_attention_wide(a, D, p.few_rows, p.wide_parts,
+                                                  workspace + p.few_bytes / 4, stream);
+    if (e != hipSuccess || !p.few) return e;
   }
-  const int nt = row_fragments(max_query * a.group, D);
-  const bool split = splits(max_seq) && workspace_bytes >= partial_bytes(D, nt);
+  const bool split = p.few_bytes > 0;
   if (D == 64)
-    return nt == 2 ? launch<64, 2>(a, split, workspace, stream)
-                   : launch<64, 1>(a, split, workspace, stream);
+    return p.nt == 2 ? launch<64, 2>(a, split, workspace, stream)
+                     : launch<64, 1>(a, split, workspace, stream);
   if (D == 128)
-    return nt == 2 ? launch<128, 2>(a, split, workspace, stream)
-                   : launch<128, 1>(a, split, workspace, stream);
+    return p.nt == 2 ? launch<128, 2>(a, split, workspace, stream)
+                     : launch<128, 1>(a, split, workspace, stream);
   return launch<256, 1>(a, split, workspace, stream);
 }
 

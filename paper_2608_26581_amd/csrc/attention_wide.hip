@@ -50,6 +50,8 @@ struct Wide {
   static constexpr int kLanes = D / 32;                   // 32-channel blocks of a token
   static constexpr int kBlocks = kTile * kLanes;          // of a tile
   static constexpr int kLoads = (kBlocks + kThreads - 1) / kThreads;
+  // With two threads for each block, one decodes the keys' and one the values'.
+  static constexpr bool kRoles = kThreads >= 2 * kBlocks;
   // In LDS the keys are rows of channels, the values rows of tokens (transposed while
   // they are decoded: a transposing read takes twice the LDS time of a plain one), with
   // the channel of row r r % (D / 8) * 8 + r / (D / 8) and the tokens in the order in which P
@@ -61,6 +63,23 @@ struct Wide {
   static constexpr int kScales = kBlocks;                 // the values' scale bytes [block][token]
   static constexpr int kLds = 2 * (kKeys + kValues + kScales);    // two tiles
 };
+
+// The request that row tile `index` is numbered for, and which of its tiles it is (there
+// may be none).
+template <class S>
+__device__ __forceinline__ int request_of_tile(const AttentionArgs &a, int index, int &rt) {
+  auto first = [&](int b) {
+    return (int)((int64_t)min(max(a.starts[b], 0), a.T) * a.group / S::kRows) + b;
+  };
+  int b = 0, past = a.B;
+  while (past - b > 1) {
+    const int mid = (b + past) >> 1;
+    if (first(mid) <= index) b = mid;
+    else past = mid;
+  }
+  rt = index - first(b);
+  return b;
+}
 
 // Requests with more than few_rows rows (the others are attention.hip's).  The row
 // tiles of request b are numbered from floor(start_b group / 128) + b, which leaves
@@ -74,7 +93,7 @@ struct Wide {
 // read, behind the tile's one barrier.
 template <int D, int NR, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attention_wide_kernel(
-    const AttentionArgs a, int few_rows, int tiles) {
+    const AttentionArgs a, int few_rows, int tiles, float *parts_o, float *parts_ml) {
   using S = Wide<D, NR, WAVES>;
   constexpr int LT = S::kLanes, KS = D / 16, CT = D / 32, L = S::kLoads;
   constexpr int kThreads = S::kThreads;
@@ -88,17 +107,10 @@ __global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attentio
   // blocks stay in one XCD's L2); the last row tiles, with the most tokens, come first.
   const int head = blockIdx.x % a.heads;
   const int index = tiles - 1 - (int)(blockIdx.x / a.heads);
-  auto first_tile = [&](int b) {
-    return (int)((int64_t)min(max(a.starts[b], 0), a.T) * a.group / S::kRows) + b;
-  };
-  int b = 0, past = a.B;
-  while (past - b > 1) {
-    const int mid = (b + past) >> 1;
-    if (first_tile(mid) <= index) b = mid;
-    else past = mid;
-  }
+  int rt;
+  const int b = request_of_tile<S>(a, index, rt);
   const Request req = request<S>(a, b);
-  const int rows = req.nq * a.group, rt = index - first_tile(b);
+  const int rows = req.nq * a.group;
   if (rows <= few_rows || rt < 0 || rt >= req.row_tiles) return;
 
   // The lane's rows, one of each 32; their queries as the right operand, and what they
@@ -132,14 +144,22 @@ __global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attentio
   const int all_hi = a.causal ? p0 : req.len - 1, all_lo = a.window ? p1 - a.window + 1 : 0;
   const int g_hi = a.causal ? position(row0 + S::kRows - 1) : req.len - 1;
   const int g_lo = a.window ? max(position(row0) - a.window + 1, 0) : 0;
-  const int tile0 = g_lo / S::kTile, end = g_hi < 0 ? 0 : g_hi / S::kTile + 1;
+  int tile0 = g_lo / S::kTile, end = g_hi < 0 ? 0 : g_hi / S::kTile + 1;
+  const int parts = gridDim.y, part = blockIdx.y;
+  if (parts > 1) {                                        // this workgroup's share of the tiles
+    const int share = (max(end - tile0, 0) + parts - 1) / parts;
+    tile0 += part * share;
+    end = min(end, tile0 + share);
+  }
 
   const int32_t *table = a.tables + (int64_t)b * a.width;
   // The thread's part of a tile.  Keys: block n % LT of token n / LT, n = tid + 256 l.
   // Values, a tile later: 8 channels n % kOctets of the 4 tokens n / kOctets, which are in
-  // the same piece of 16 tokens as its keys.  (Where a tile has fewer than 256 of them, two
-  // threads do the same.)
-  const int first_n = S::kBlocks < kThreads ? tid % S::kBlocks : tid;
+  // the same piece of 16 tokens as its keys.
+  static_assert(S::kRoles || S::kBlocks % kThreads == 0, "every thread has the same work");
+  const int first_n = S::kRoles ? tid % S::kBlocks : tid;
+  const bool keys_mine = !S::kRoles || wave < S::kBlocks / 64;
+  const bool values_mine = !S::kRoles || !keys_mine;
   u32x4 kc[L], vc[L];                                     // vc: a token's 8 codes each
   uint32_t ks[L], vs[L];
   const uint32_t *v_from[L];
@@ -161,15 +181,18 @@ __global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attentio
       ok[l] = (uint32_t)id[l] < (uint32_t)a.blocks;
       const int64_t row = (((int64_t)(ok[l] ? id[l] : 0) * a.heads + head) << a.page_shift) +
                           ((tile * S::kTile + (token & ~15)) & (a.page - 1));
-      const int64_t at = (row + (token & 15)) * LT + n % LT;
-      kc[l] = reinterpret_cast<const u32x4 *>(a.k_codes)[at];
-      ks[l] = a.k_scales[at];
-      vs[l] = a.v_scales[at];
+      if (keys_mine) {
+        const int64_t at = (row + (token & 15)) * LT + n % LT;
+        kc[l] = reinterpret_cast<const u32x4 *>(a.k_codes)[at];
+        ks[l] = a.k_scales[at];
+        vs[l] = a.v_scales[at];
+      }
       v_from[l] = reinterpret_cast<const uint32_t *>(a.v_codes) +
                   (row + (quad & 15)) * S::kOctets + n % S::kOctets;
     }
   };
   auto fetch_values = [&] {
+    if (!values_mine) return;
 #pragma unroll
     for (int l = 0; l < L; ++l)
 #pragma unroll
@@ -179,6 +202,7 @@ __global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attentio
   // that bf16 does not hold) makes its token's scores NaN; the values in LDS are finite,
   // so that a masked P gives 0.
   auto decode_key = [&](int buf, int tile, int l, int w) {
+    if (!keys_mine) return;
     const int n = first_n + kThreads * l, token = n / LT, block = n % LT;
     u32x4 x = decode_bf16(kc[l][w], scale_operand(ks[l]));
     if (w == 0) {
@@ -190,6 +214,7 @@ __global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attentio
         x;
   };
   auto decode_value = [&](int buf, int l, int w) {
+    if (!values_mine) return;
     const int n = first_n + kThreads * l, octet = n % S::kOctets, quad = n / S::kOctets;
     if (w == 0) {
       const uint32_t scales = *reinterpret_cast<const uint32_t *>(
@@ -370,8 +395,15 @@ __global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attentio
         // The next codes to LDS, keys first; then the loads that take their registers.
 #pragma unroll
         for (int x = k * 8 * L / KS; x < (k + 1) * 8 * L / KS; ++x) {
-          if (x < 4 * L) decode_key(buf, tile + 2, x / 4, x % 4);
-          else decode_value(buf ^ 1, x / 4 - L, x % 4);
+          if constexpr (S::kRoles) {
+            if (x % 2 == 0) {
+              decode_key(buf, tile + 2, x / 8, x / 2 % 4);
+              decode_value(buf ^ 1, x / 8, x / 2 % 4);
+            }
+          } else {
+            if (x < 4 * L) decode_key(buf, tile + 2, x / 4, x % 4);
+            else decode_value(buf ^ 1, x / 4 - L, x % 4);
+          }
         }
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -404,6 +436,23 @@ __global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attentio
     const float l = __uint_as_float(both[0]) + __uint_as_float(both[1]);
     const int r = w0 + 32 * n + col, i = r / a.group, qh = head * a.group + (r - i * a.group);
     if (r >= rows) continue;
+    if (parts > 1) {
+      const int64_t at = ((int64_t)(index * a.heads + head) * parts + part) * S::kRows + r - row0;
+      if (h == 0) {
+        parts_ml[2 * at] = m[n];
+        parts_ml[2 * at + 1] = l;
+      }
+      // Elements in the registers' order (the join's threads each take one position).
+#pragma unroll
+      for (int t = 0; t < CT; ++t)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const v16f &x = o[n][t];
+          *reinterpret_cast<v4f *>(parts_o + at * D + 32 * t + 8 * q + 4 * h) =
+              v4f{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+        }
+      continue;
+    }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     uint16_t *out = a.out + (req.start + i) * a.o_ts + qh * a.o_hs;
     // Element e of tile t is row 32 t + 8 (e / 4) + 4 h + e % 4: 8 channels in the order of
@@ -431,25 +480,83 @@ __global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attentio
   }
 }
 
+// The parts of the row tiles joined, in their order: thread = (row, 4 of the LDS rows that
+// the channels have there).
 template <int D, int NR, int WAVES>
-hipError_t launch(const AttentionArgs &a, int few_rows, hipStream_t stream) {
+__global__ __launch_bounds__(256) void kv_attention_wide_join_kernel(
+    const AttentionArgs a, int few_rows, int tiles, int parts, const float *parts_o,
+    const float *parts_ml) {
+  using S = Wide<D, NR, WAVES>;
+  constexpr int kLanes = D / 4, kRowsHere = 256 / kLanes;
+  const int head = blockIdx.x % a.heads, index = blockIdx.x / a.heads;
+  if (index >= tiles) return;
+  int rt;
+  const int b = request_of_tile<S>(a, index, rt);
+  const Request req = request<S>(a, b);
+  const int rows = req.nq * a.group;
+  const int row = blockIdx.y * kRowsHere + threadIdx.x / kLanes, r = rt * S::kRows + row;
+  if (rows <= few_rows || rt < 0 || rt >= req.row_tiles || r >= rows) return;
+  const int c = threadIdx.x % kLanes * 4;
+  const int64_t first = (int64_t)(index * a.heads + head) * parts * S::kRows + row;
+  float top = neg_inf();
+  for (int i = 0; i < parts; ++i) top = fmaxf(top, parts_ml[2 * (first + (int64_t)i * S::kRows)]);
+  const float ref = top == neg_inf() ? 0.0f : top;
+  float l = 0.0f;
+  v4f x = {0, 0, 0, 0};
+  for (int i = 0; i < parts; ++i) {
+    const int64_t at = first + (int64_t)i * S::kRows;
+    const float f = exp2_hw(parts_ml[2 * at] - ref);
+    l += parts_ml[2 * at + 1] * f;
+    x += *reinterpret_cast<const v4f *>(parts_o + at * D + c) * f;
+  }
+  x *= l == 0.0f ? 0.0f : 1.0f / l;
+  const int i = r / a.group, qh = head * a.group + (r - i * a.group);
+  uint16_t *out = a.out + (req.start + i) * a.o_ts + qh * a.o_hs;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int lds_row = c + e;
+    const __bf16 y = (__bf16)x[e];
+    out[lds_row % S::kOctets * 8 + lds_row / S::kOctets] = __builtin_bit_cast(uint16_t, y);
+  }
+  if (a.lse && c == 0)
+    a.lse[(int64_t)(req.start + i) * a.Hq + qh] =
+        l == 0.0f ? neg_inf() : (top + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+template <int D, int NR, int WAVES>
+hipError_t launch(const AttentionArgs &a, int few_rows, int parts, float *work,
+                  hipStream_t stream) {
   using S = Wide<D, NR, WAVES>;
   static std::atomic<bool> limit[kMaxDevices];
   const auto kernel = kv_attention_wide_kernel<D, NR, WAVES>;
-  const hipError_t e = set_lds_limit(limit, (const void *)kernel, S::kLds);
+  hipError_t e = set_lds_limit(limit, (const void *)kernel, S::kLds);
   if (e != hipSuccess) return e;
-  const int64_t tiles = (int64_t)a.T * a.group / S::kRows + a.B;
-  kernel<<<(unsigned)(tiles * a.heads), S::kThreads, S::kLds, stream>>>(a, few_rows, (int)tiles);
+  const int64_t tiles = wide_tiles(a.T, a.group, a.B), items = tiles * a.heads;
+  float *ml = work ? work + items * parts * S::kRows * D : nullptr;
+  kernel<<<dim3((unsigned)items, (unsigned)parts), S::kThreads, S::kLds, stream>>>(
+      a, few_rows, (int)tiles, work, ml);
+  if ((e = hipGetLastError()) != hipSuccess || parts == 1) return e;
+  kv_attention_wide_join_kernel<D, NR, WAVES>
+      <<<dim3((unsigned)items, (unsigned)(S::kRows * D / 4 / 256)), 256, 0, stream>>>(
+          a, few_rows, (int)tiles, parts, work, ml);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_kv_attention_wide(const AttentionArgs &a, int64_t D, int few_rows,
-                                    hipStream_t stream) {
-  if (D == 64) return launch<64, 1, 4>(a, few_rows, stream);
-  if (D == 128) return launch<128, 1, 4>(a, few_rows, stream);
-  return launch<256, 1, 4>(a, few_rows, stream);
+int64_t wide_tiles(int64_t T, int64_t group, int64_t B) {
+  return T * group / kWideRows + B;
+}
+
+int64_t wide_bytes(int64_t items, int parts, int64_t D) {
+  return parts > 1 ? items * parts * kWideRows * (D + 2) * (int64_t)sizeof(float) : 0;
+}
+
+hipError_t launch_kv_attention_wide(const AttentionArgs &a, int64_t D, int few_rows, int parts,
+                                    float *work, hipStream_t stream) {
+  if (D == 64) return launch<64, 1, 4>(a, few_rows, parts, work, stream);
+  if (D == 128) return launch<128, 1, 4>(a, few_rows, parts, work, stream);
+  return launch<256, 1, 4>(a, few_rows, parts, work, stream);
 }
 
 }  // namespace rfq

@@ -57,9 +57,14 @@ struct AttentionArgs {
 };
 int64_t kv_attention_workspace(int64_t T, int64_t Hq, int64_t heads, int64_t D, int64_t B,
                                int64_t max_query, int64_t max_seq);
-// The wide kernel: requests with more than few_rows rows (queries times group).
-hipError_t launch_kv_attention_wide(const AttentionArgs &args, int64_t D, int few_rows,
-                                    hipStream_t stream);
+// The wide kernel: requests with more than few_rows rows (queries times group), in row
+// tiles of kWideRows (at most wide_tiles a head); their tokens in `parts` parts, with
+// parts > 1 in wide_bytes(tiles * heads) of workspace.
+constexpr int kWideRows = 128;
+int64_t wide_tiles(int64_t T, int64_t group, int64_t B);
+int64_t wide_bytes(int64_t items, int parts, int64_t D);
+hipError_t launch_kv_attention_wide(const AttentionArgs &args, int64_t D, int few_rows, int parts,
+                                    float *work, hipStream_t stream);
 hipError_t launch_kv_attention(const AttentionArgs &args, int64_t D, int64_t max_query,
                                int64_t max_seq, float *workspace, int64_t workspace_bytes,
                                hipStream_t stream);

@@ -94,6 +94,17 @@ def test_many_rows(D, reqs, causal, window):
     _check(rng, reqs, 128, 64, D, 16, causal=causal, window=window)
 
 
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("window", [0, 700, 1500])
+@pytest.mark.parametrize("causal", [True, False])
+def test_many_rows_split(D, window, causal):
+    """Few row tiles over long histories: the tokens in parts, some of them empty."""
+    rng = np.random.default_rng(D + window)
+    _check(rng, [(4600, 40), (2500, 1), (2100, 70), (0, 33), (30, 30)], 8, 2, D, 64, causal=causal,
+           window=window)
+    _check(rng, [(3000, 20)], 10, 2, D, 16, causal=causal, window=window)
+
+
 @pytest.mark.parametrize("group,heads,page", [(1, 128, 32), (3, 48, 128), (7, 20, 64), (20, 8, 256)])
 def test_many_rows_groups(group, heads, page):
     rng = np.random.default_rng(group)
