@@ -28,8 +28,9 @@
 namespace rfq {
 namespace {
 
-// Workgroups that the split kernel's work is divided over: two per CU.
-constexpr int kSplitGroups = 512;
+// Workgroups that the split kernel's work is divided over: three per CU where the
+// registers allow three waves a SIMD, else two.
+constexpr int split_groups(int64_t D, int nt) { return D <= 128 && nt == 1 ? 768 : 512; }
 // An item's queries, its first loads and the joining of the waves take about as long
 // as this many tiles.
 constexpr int kItemCost = 4;
@@ -564,19 +565,20 @@ int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int row_fragments(int64_t rows, int64_t D) { return D < 256 && rows > 16 ? 2 : 1; }
 
 int64_t partial_bytes(int64_t D, int nt) {
-  return (int64_t)kSplitGroups * (2 * 16 * nt * (D + 2) * 4 + 16);
+  return (int64_t)split_groups(D, nt) * (2 * 16 * nt * (D + 2) * 4 + 16);
 }
 
 template <int D, int NT>
 hipError_t launch(const AttentionArgs &a, bool split, float *work, hipStream_t stream) {
   using S = Shape<D, NT>;
+  constexpr int kGroups = split_groups(D, NT);
   Partial p = {};
   unsigned grid;
   if (split) {
     p.o = work;
-    p.ml = work + (int64_t)kSplitGroups * 2 * S::kRows * D;
-    p.item = reinterpret_cast<int4 *>(p.ml + (int64_t)kSplitGroups * 2 * S::kRows * 2);
-    grid = kSplitGroups;
+    p.ml = work + (int64_t)kGroups * 2 * S::kRows * D;
+    p.item = reinterpret_cast<int4 *>(p.ml + (int64_t)kGroups * 2 * S::kRows * 2);
+    grid = kGroups;
   } else {
     // At least as many workgroups as there are items, within a launch's limits.
     const int64_t items = (up((int64_t)a.T * a.group, S::kRows) + a.B) * a.heads;
@@ -585,7 +587,7 @@ hipError_t launch(const AttentionArgs &a, bool split, float *work, hipStream_t s
   kv_attention_kernel<D, NT><<<grid, kThreads, 0, stream>>>(a, p, split);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !split) return e;
-  const dim3 join(kSplitGroups, (unsigned)up(S::kRows, kThreads / (D / 4)));
+  const dim3 join(kGroups, (unsigned)up(S::kRows, kThreads / (D / 4)));
   kv_attention_join_kernel<D, NT><<<join, kThreads, 0, stream>>>(a, p);
   return hipGetLastError();
 }
