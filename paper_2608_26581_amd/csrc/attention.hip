@@ -40,13 +40,13 @@ constexpr int64_t kLeastPart = 1024;
 
 // ---- the shapes and the requests
 
-template <int D, int NT>
+// D channels, NT 16-row fragments, P 16-token pieces a step of a wave.  Long work takes
+// P = 4 (4 requests of 131072 tokens 119 us, with 2 126), little work P = 2, whose steps more
+// waves share (one request of 700 tokens 8.6 us, with 4 11.7), and so do 256 channels, whose
+// codes would not fit the registers otherwise.
+template <int D, int NT, int P>
 struct Shape {
-  static constexpr int kRows = 16 * NT;
-  // Tokens of a wave's step, in pieces of 16: the codes of two steps are in
-  // registers (at 64 tokens of 256 channels they would be spilled).
-  static constexpr int kPieces = D == 256 ? 2 : 4;
-  static constexpr int kTile = 16 * kPieces;
+  static constexpr int kRows = 16 * NT, kPieces = P, kTile = 16 * P;
   static constexpr int kWords = D / 32;                  // code dwords of a lane and token
   static constexpr int kLoads = kTile * D / 2 / 1024;    // 16-byte loads of a tile's codes
   static constexpr int kLanes = D / 32;                  // lanes of a token in a load
@@ -70,7 +70,11 @@ __device__ __forceinline__ int64_t units(const AttentionArgs &a, const Request &
 struct Partial {
   float *o;                               // [groups * 2][ROWS][D]
   float *ml;                              // [groups * 2][ROWS][2]
-  int4 *item;                             // [groups] item whose first part ends the range
+  struct Item {
+    int start, row0, rows, head;          // the request's first row of q; of its rows row0 on
+    int parts;                            // 0: no such item
+    int unused[3];
+  } *item;                                // [groups] item whose first part ends the range
 };
 
 // A lane's part of a tile.  Codes of 1 KB a load, 16 bytes a lane in the order of
@@ -83,12 +87,12 @@ struct Codes {
   uint32_t ks[S::kPieces];                // 256 channels: two bytes
 };
 
-template <int D, int NT>
+template <int D, int NT, int P>
 __global__ __launch_bounds__(kThreads, NT == 1 && D <= 128 ? 3 : 2) void kv_attention_kernel(const AttentionArgs a,
                                                                    const Partial part,
                                                                    int split) {
-  using S = Shape<D, NT>;
-  constexpr int W = S::kWords, P = S::kPieces;
+  using S = Shape<D, NT, P>;
+  constexpr int W = S::kWords;
   __shared__ alignas(16) uint8_t lds_v[kWaves][S::kWaveLds];
   __shared__ float lds_ml[kWaves][S::kRows][2];
   __shared__ int64_t scan[kWaves];
@@ -163,7 +167,7 @@ __global__ __launch_bounds__(kThreads, NT == 1 && D <= 128 ? 3 : 2) void kv_atte
     base = lane_value(found_at, 0);
     hold(b);
   }
-  if (part.item && tid == 0) part.item[wg] = make_int4(0, 0, 0, 0);
+  if (part.item && tid == 0) part.item[wg].parts = 0;
   if (u0 >= u1) return;
   auto pick = [&](int i) {                // request i, of those held
     if (i >= held + 64) hold(i);
@@ -499,7 +503,7 @@ __global__ __launch_bounds__(kThreads, NT == 1 && D <= 128 ? 3 : 2) void kv_atte
     if (!complete && first && tid == 0) {
       // Its other parts are the first of the following workgroups' ranges.
       const int parts = 1 + (int)((nk - k1 + share - 1) / share);
-      part.item[wg] = make_int4(b, head, rt, parts);
+      part.item[wg] = {req.start, row0, rows, head, parts, {}};
     }
   }
 }
@@ -510,52 +514,56 @@ __global__ __launch_bounds__(kThreads, NT == 1 && D <= 128 ? 3 : 2) void kv_atte
 template <int D, int NT>
 __global__ __launch_bounds__(kThreads) void kv_attention_join_kernel(const AttentionArgs a,
                                                                      const Partial part) {
-  using S = Shape<D, NT>;
+  constexpr int kRows = 16 * NT, kLanes = D / 4;         // kLanes: threads of a row
   const int wg = blockIdx.x;
-  const int4 it = part.item[wg];
-  if (it.w == 0) return;
-  const Request req = request<S>(a, it.x);
-  constexpr int kLanes = D / 4;                          // threads of a row
-  const int row = blockIdx.y * (kThreads / kLanes) + threadIdx.x / kLanes;
-  const int r = it.z * S::kRows + row;
-  if (r >= req.nq * a.group) return;
+  const Partial::Item it = part.item[wg];
+  const int n = it.parts;
+  const int row = blockIdx.y * (kThreads / kLanes) + threadIdx.x / kLanes, r = it.row0 + row;
+  if (n == 0 || r >= it.rows) return;
   const int lr = threadIdx.x % kLanes, c = 4 * lr;
-  auto slot = [&](int i) { return (int64_t)(i == 0 ? 2 * wg + 1 : 2 * (wg + i)) * S::kRows + row; };
-  // A lane of the row takes every kLanes-th part's statistics.
+  auto slot = [&](int i) { return (int64_t)(i == 0 ? 2 * wg + 1 : 2 * (wg + i)) * kRows + row; };
+  // A lane of the row takes the statistics of every kLanes-th part; the first parts'
+  // sums are on their way meanwhile.
+  constexpr int kBatch = 8;
+  v4f y[kBatch];
+  auto fetch = [&](int i0) {
+#pragma unroll
+    for (int e = 0; e < kBatch; ++e)
+      y[e] = *reinterpret_cast<const v4f *>(part.o + slot(min(i0 + e, n - 1)) * D + c);
+  };
   float top = neg_inf();
-  for (int i = lr; i < it.w; i += kLanes) top = fmaxf(top, part.ml[slot(i) * 2]);
+  for (int i = lr; i < n; i += kLanes) top = fmaxf(top, part.ml[slot(i) * 2]);
+  fetch(0);
 #pragma unroll
   for (int d = 1; d < kLanes; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
   const float ref = top == neg_inf() ? 0.0f : top;
-  float sum = 0.0f;
+  float sum = 0.0f, f = 0.0f;
   v4f x = {0, 0, 0, 0};
-  for (int i0 = 0; i0 < it.w; i0 += kLanes) {
-    float f = 0.0f;
-    if (i0 + lr < it.w) {
-      const float *ml = part.ml + slot(i0 + lr) * 2;
-      f = exp2_hw(ml[0] - ref);
-      sum += ml[1] * f;
+  for (int i0 = 0; i0 < n; i0 += kBatch) {
+    if (i0 % kLanes == 0) {
+      f = 0.0f;
+      if (i0 + lr < n) {
+        const float *ml = part.ml + slot(i0 + lr) * 2;
+        f = exp2_hw(ml[0] - ref);
+        sum += ml[1] * f;
+      }
     }
-    constexpr int kBatch = 8;                            // loads in flight
-    for (int i = 0; i < min(kLanes, it.w - i0); i += kBatch) {
-      v4f y[kBatch];
 #pragma unroll
-      for (int e = 0; e < kBatch; ++e)
-        y[e] = *reinterpret_cast<const v4f *>(part.o + slot(min(i0 + i + e, it.w - 1)) * D + c);
-#pragma unroll
-      for (int e = 0; e < kBatch; ++e)
-        if (i0 + i + e < it.w) x += y[e] * __shfl(f, i + e, kLanes);
+    for (int e = 0; e < kBatch; ++e) {
+      const float w = __shfl(f, (i0 + e) % kLanes, kLanes);
+      if (i0 + e < n) x += y[e] * w;
     }
+    if (i0 + kBatch < n) fetch(i0 + kBatch);
   }
 #pragma unroll
   for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor(sum, d);
   x *= sum == 0.0f ? 0.0f : 1.0f / sum;
-  const int i = r / a.group, h = it.y * a.group + (r - i * a.group);
-  const bf16x4 y = {(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
-  *reinterpret_cast<u32x2 *>(a.out + (req.start + i) * a.o_ts + h * a.o_hs + c) =
-      __builtin_bit_cast(u32x2, y);
+  const int i = r / a.group, h = it.head * a.group + (r - i * a.group);
+  const bf16x4 z = {(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+  *reinterpret_cast<u32x2 *>(a.out + (it.start + i) * a.o_ts + h * a.o_hs + c) =
+      __builtin_bit_cast(u32x2, z);
   if (a.lse && c == 0)
-    a.lse[(int64_t)(req.start + i) * a.Hq + h] =
+    a.lse[(int64_t)(it.start + i) * a.Hq + h] =
         sum == 0.0f ? neg_inf() : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
@@ -565,26 +573,26 @@ int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int row_fragments(int64_t rows, int64_t D) { return D < 256 && rows > 16 ? 2 : 1; }
 
 int64_t partial_bytes(int64_t D, int nt) {
-  return (int64_t)split_groups(D, nt) * (2 * 16 * nt * (D + 2) * 4 + 16);
+  return (int64_t)split_groups(D, nt) * (2 * 16 * nt * (D + 2) * 4 + (int64_t)sizeof(Partial::Item));
 }
 
-template <int D, int NT>
+template <int D, int NT, int P>
 hipError_t launch(const AttentionArgs &a, bool split, float *work, hipStream_t stream) {
-  using S = Shape<D, NT>;
+  using S = Shape<D, NT, P>;
   constexpr int kGroups = split_groups(D, NT);
   Partial p = {};
   unsigned grid;
   if (split) {
     p.o = work;
     p.ml = work + (int64_t)kGroups * 2 * S::kRows * D;
-    p.item = reinterpret_cast<int4 *>(p.ml + (int64_t)kGroups * 2 * S::kRows * 2);
+    p.item = reinterpret_cast<Partial::Item *>(p.ml + (int64_t)kGroups * 2 * S::kRows * 2);
     grid = kGroups;
   } else {
     // At least as many workgroups as there are items, within a launch's limits.
     const int64_t items = (up((int64_t)a.T * a.group, S::kRows) + a.B) * a.heads;
     grid = (unsigned)(items < kMaxGrid ? items : kMaxGrid);
   }
-  kv_attention_kernel<D, NT><<<grid, kThreads, 0, stream>>>(a, p, split);
+  kv_attention_kernel<D, NT, P><<<grid, kThreads, 0, stream>>>(a, p, split);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !split) return e;
   const dim3 join(kGroups, (unsigned)up(S::kRows, kThreads / (D / 4)));
@@ -651,13 +659,19 @@ hipError_t launch_kv_attention(const AttentionArgs &args, int64_t D, int64_t max
     if (e != hipSuccess || !p.few) return e;
   }
   const bool split = p.few_bytes > 0;
-  if (D == 64)
-    return p.nt == 2 ? launch<64, 2>(a, split, workspace, stream)
-                     : launch<64, 1>(a, split, workspace, stream);
-  if (D == 128)
-    return p.nt == 2 ? launch<128, 2>(a, split, workspace, stream)
-                     : launch<128, 1>(a, split, workspace, stream);
-  return launch<256, 1>(a, split, workspace, stream);
+  // Little work: at most four steps of 64 tokens for each wave that is resident.
+  const bool little = max_seq <= (int64_t(4) * 64 * 3072) / ((int64_t)a.B * a.heads);
+  if (D == 64) {
+    if (p.nt == 2) return launch<64, 2, 4>(a, split, workspace, stream);
+    return little ? launch<64, 1, 2>(a, split, workspace, stream)
+                  : launch<64, 1, 4>(a, split, workspace, stream);
+  }
+  if (D == 128) {
+    if (p.nt == 2) return launch<128, 2, 4>(a, split, workspace, stream);
+    return little ? launch<128, 1, 2>(a, split, workspace, stream)
+                  : launch<128, 1, 4>(a, split, workspace, stream);
+  }
+  return launch<256, 1, 2>(a, split, workspace, stream);
 }
 
 }  // namespace rfq
