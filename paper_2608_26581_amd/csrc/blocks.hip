@@ -18,6 +18,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "kv.h"
 #include "rfq_internal.h"
@@ -25,10 +26,12 @@
 namespace rfq {
 namespace {
 
-constexpr int kThreads = 256;
+// Workgroups of 256 work items, or with many requests of 1024: a request's lengths are a
+// round trip to L2 apart where a thread has several (2000 requests, 126000 tokens: 12.7 us
+// with 256, 8.0 with 1024 and loads in fours).
+constexpr int kFewThreads = 256, kManyThreads = 1024;
 constexpr int kTokensPerGroup = 1024;
-constexpr int kEntriesPerGroup = 1024;
-std::atomic<bool> g_lds_assign[kMaxDevices], g_lds_release[kMaxDevices];
+constexpr int kBatch = 4;                   // requests whose lengths are loaded together
 
 __device__ __forceinline__ int64_t wave_inclusive(int64_t v) {
   const int lane = threadIdx.x & 63;
@@ -40,8 +43,9 @@ __device__ __forceinline__ int64_t wave_inclusive(int64_t v) {
   return v;
 }
 
-// Exclusive prefix over the workgroup's threads; total: the sum.  part: 4 values
-// of LDS that nothing else uses until the next barrier.
+// Exclusive prefix over the workgroup's threads; total: the sum.  part: a value of LDS
+// for each wave, that nothing else uses until the next barrier.
+template <int kThreads>
 __device__ __forceinline__ int64_t group_exclusive(int64_t v, int64_t *part, int64_t &total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t incl = wave_inclusive(v);
@@ -49,7 +53,6 @@ __device__ __forceinline__ int64_t group_exclusive(int64_t v, int64_t *part, int
   __syncthreads();
   int64_t before = 0;
   total = 0;
-#pragma unroll
   for (int w = 0; w < kThreads / 64; ++w) {
     if (w < wave) before += part[w];
     total += part[w];
@@ -75,6 +78,7 @@ __device__ __forceinline__ int owner(const int32_t *start, int n, int64_t t) {
   return lo;
 }
 
+template <int kThreads>
 __global__ __launch_bounds__(kThreads) void block_assign_kernel(
     const int32_t *__restrict__ ctx_lens, const int32_t *__restrict__ new_lens, int B,
     int32_t *tables, int64_t width, const int32_t *__restrict__ free_blocks, int64_t n_free,
@@ -90,44 +94,59 @@ __global__ __launch_bounds__(kThreads) void block_assign_kernel(
   const int64_t page1 = (int64_t(1) << page_shift) - 1;
   const int64_t count = clamped(free_count[0], 0, n_free);
 
-  auto lengths = [&](int b, int64_t &ctx, int64_t &add, int64_t &held, int64_t &extra,
-                     bool &fits) {
-    ctx = max(ctx_lens[b], 0);
-    add = max(new_lens[b], 0);
-    held = (ctx + page1) >> page_shift;
-    const int64_t need = (ctx + add + page1) >> page_shift;
-    fits = need <= width && ctx + add <= INT32_MAX;
-    extra = fits ? need - held : 0;
+  struct Lengths {
+    int64_t ctx, add, extra;
+    bool fits;
+  };
+  // f(b, lengths) for the thread's requests in their order, kBatch loaded at a time.
+  auto each = [&](auto f) {
+    for (int i = b0; i < b1; i += kBatch) {
+      int32_t c[kBatch], n[kBatch];
+#pragma unroll
+      for (int e = 0; e < kBatch; ++e) {
+        c[e] = ctx_lens[min(i + e, b1 - 1)];
+        n[e] = new_lens[min(i + e, b1 - 1)];
+      }
+#pragma unroll
+      for (int e = 0; e < kBatch; ++e) {
+        if (i + e >= b1) break;
+        Lengths l;
+        l.ctx = max(c[e], 0);
+        l.add = max(n[e], 0);
+        const int64_t held = (l.ctx + page1) >> page_shift;
+        const int64_t need = (l.ctx + l.add + page1) >> page_shift;
+        l.fits = need <= width && l.ctx + l.add <= INT32_MAX;
+        l.extra = l.fits ? need - held : 0;
+        f(i + e, l);
+      }
+    }
   };
 
-  int64_t ctx, add, held, extra, ntok = 0, nblk = 0, all_tok, all_blk;
-  bool fits;
-  for (int b = b0; b < b1; ++b) {
-    lengths(b, ctx, add, held, extra, fits);
-    ntok += add;
-    nblk += extra;
-  }
-  int64_t s = group_exclusive(ntok, part[0], all_tok);
-  int64_t f = group_exclusive(nblk, part[1], all_blk);
+  int64_t ntok = 0, nblk = 0, all_tok, all_blk;
+  each([&](int, const Lengths &l) {
+    ntok += l.add;
+    nblk += l.extra;
+  });
+  int64_t s = group_exclusive<kThreads>(ntok, part[0], all_tok);
+  int64_t f = group_exclusive<kThreads>(nblk, part[1], all_blk);
   // Taken blocks: the requests served form a prefix of those that lack blocks, so
   // their sum is the largest end of one that is served.
   int64_t taken = 0;
   int refused = 0;
   const bool leader = blockIdx.x == 0;
-  for (int b = b0; b < b1; ++b) {
-    lengths(b, ctx, add, held, extra, fits);
-    const bool ok = fits && (extra == 0 || f + extra <= count);
+  each([&](int b, const Lengths &l) {
+    const bool ok = l.fits && (l.extra == 0 || f + l.extra <= count);
     start[b] = saturated(s);
     first[b] = ok ? saturated(f) : -1;
-    if (ok && extra > 0) taken = f + extra;
+    if (ok && l.extra > 0) taken = f + l.extra;
     refused += !ok;
     if (leader) {
       query_starts[b] = saturated(s);
-      seq_lens[b] = ok ? (int32_t)(ctx + add) : 0;
+      seq_lens[b] = ok ? (int32_t)(l.ctx + l.add) : 0;
     }
-    s += add;
-    f += extra;
-  }
+    s += l.add;
+    f += l.extra;
+  });
   if (leader) {
     int64_t served = taken, no = refused;
 #pragma unroll
@@ -155,7 +174,6 @@ __global__ __launch_bounds__(kThreads) void block_assign_kernel(
   }
 
   const int64_t t0 = (int64_t)blockIdx.x * kTokensPerGroup;
-#pragma unroll
   for (int i = 0; i < kTokensPerGroup / kThreads; ++i) {
     const int64_t t = t0 + i * kThreads + tid;
     if (t >= tokens) break;
@@ -181,6 +199,7 @@ __global__ __launch_bounds__(kThreads) void block_assign_kernel(
   }
 }
 
+template <int kThreads>
 __global__ __launch_bounds__(kThreads) void block_release_kernel(
     const int32_t *__restrict__ lens, const uint8_t *__restrict__ ended, int B,
     const int32_t *__restrict__ tables, int64_t width, int32_t *__restrict__ free_blocks,
@@ -192,17 +211,30 @@ __global__ __launch_bounds__(kThreads) void block_release_kernel(
   const int b0 = tid * per, b1 = min(B, b0 + per);
   const int64_t page1 = (int64_t(1) << page_shift) - 1;
   const int64_t count = clamped(free_count[0], 0, n_free);
-  auto given = [&](int b) {
-    const int64_t n = (max((int64_t)lens[b], (int64_t)0) + page1) >> page_shift;
-    return ended[b] ? (n < width ? n : width) : (int64_t)0;
+  auto each = [&](auto f) {
+    for (int i = b0; i < b1; i += kBatch) {
+      int32_t len[kBatch];
+      uint8_t end[kBatch];
+#pragma unroll
+      for (int e = 0; e < kBatch; ++e) {
+        len[e] = lens[min(i + e, b1 - 1)];
+        end[e] = ended[min(i + e, b1 - 1)];
+      }
+#pragma unroll
+      for (int e = 0; e < kBatch; ++e) {
+        if (i + e >= b1) break;
+        const int64_t n = (max((int64_t)len[e], (int64_t)0) + page1) >> page_shift;
+        f(i + e, end[e] ? (n < width ? n : width) : (int64_t)0);
+      }
+    }
   };
   int64_t n = 0, all;
-  for (int b = b0; b < b1; ++b) n += given(b);
-  int64_t f = group_exclusive(n, part, all);
-  for (int b = b0; b < b1; ++b) {
+  each([&](int, int64_t given) { n += given; });
+  int64_t f = group_exclusive<kThreads>(n, part, all);
+  each([&](int b, int64_t given) {
     lds[b] = saturated(f);
-    f += given(b);
-  }
+    f += given;
+  });
   __syncthreads();
   const int64_t room = n_free - count, copied = all < room ? all : room;
   if (blockIdx.x == 0 && tid == 0) count_out[0] = saturated(count + copied);
@@ -215,6 +247,13 @@ __global__ __launch_bounds__(kThreads) void block_release_kernel(
 
 int log2_of(int page) { return __builtin_ctz((unsigned)page); }
 
+// f<threads>() for this many requests.
+template <class F>
+hipError_t with_threads(int B, F f) {
+  return B > kFewThreads ? f(std::integral_constant<int, kManyThreads>{})
+                         : f(std::integral_constant<int, kFewThreads>{});
+}
+
 }  // namespace
 
 hipError_t launch_block_assign(const int32_t *ctx, const int32_t *fresh, int B, int32_t *tables,
@@ -222,31 +261,39 @@ hipError_t launch_block_assign(const int32_t *ctx, const int32_t *fresh, int B, 
                                const int32_t *free_count, int page, int64_t tokens,
                                int32_t *slots, int32_t *positions, int32_t *seq_lens,
                                int32_t *query_starts, int32_t *counts, hipStream_t stream) {
-  const int bytes = (int)(2 * sizeof(int32_t) * (B > 0 ? B : 1));
-  const hipError_t e = set_lds_limit(g_lds_assign, (const void *)block_assign_kernel,
-                                     (int)(2 * sizeof(int32_t) * kMaxBlockRequests));
-  if (e != hipSuccess) return e;
   const int64_t groups = (tokens + kTokensPerGroup - 1) / kTokensPerGroup;
-  block_assign_kernel<<<(unsigned)(groups > 0 ? groups : 1), kThreads, bytes, stream>>>(
-      ctx, fresh, B, tables, width, free_blocks, n_free, free_count, log2_of(page), tokens, slots,
-      positions, seq_lens, query_starts, counts);
-  return hipGetLastError();
+  return with_threads(B, [&](auto threads) {
+    constexpr int kThreads = decltype(threads)::value;
+    static std::atomic<bool> limit[kMaxDevices];
+    const auto kernel = block_assign_kernel<kThreads>;
+    const hipError_t e = set_lds_limit(limit, (const void *)kernel,
+                                       (int)(2 * sizeof(int32_t) * kMaxBlockRequests));
+    if (e != hipSuccess) return e;
+    kernel<<<(unsigned)(groups > 0 ? groups : 1), kThreads, 2 * sizeof(int32_t) * (B > 0 ? B : 1),
+             stream>>>(ctx, fresh, B, tables, width, free_blocks, n_free, free_count,
+                       log2_of(page), tokens, slots, positions, seq_lens, query_starts, counts);
+    return hipGetLastError();
+  });
 }
 
 hipError_t launch_block_release(const int32_t *lens, const uint8_t *ended, int B,
                                 const int32_t *tables, int64_t width, int32_t *free_blocks,
                                 int64_t n_free, const int32_t *free_count, int page,
                                 int32_t *count_out, hipStream_t stream) {
-  const int bytes = (int)(sizeof(int32_t) * (B > 0 ? B : 1));
-  const hipError_t e = set_lds_limit(g_lds_release, (const void *)block_release_kernel,
-                                     (int)(sizeof(int32_t) * kMaxBlockRequests));
-  if (e != hipSuccess) return e;
   const int64_t entries = B * width < n_free ? B * width : n_free;
-  int64_t groups = (entries + kEntriesPerGroup - 1) / kEntriesPerGroup;
-  groups = groups < 1 ? 1 : (groups > 256 ? 256 : groups);
-  block_release_kernel<<<(unsigned)groups, kThreads, bytes, stream>>>(
-      lens, ended, B, tables, width, free_blocks, n_free, free_count, log2_of(page), count_out);
-  return hipGetLastError();
+  return with_threads(B, [&](auto threads) {
+    constexpr int kThreads = decltype(threads)::value;
+    static std::atomic<bool> limit[kMaxDevices];
+    const auto kernel = block_release_kernel<kThreads>;
+    const hipError_t e = set_lds_limit(limit, (const void *)kernel,
+                                       (int)(sizeof(int32_t) * kMaxBlockRequests));
+    if (e != hipSuccess) return e;
+    int64_t groups = (entries + kThreads - 1) / kThreads;
+    groups = groups < 1 ? 1 : (groups > 256 ? 256 : groups);
+    kernel<<<(unsigned)groups, kThreads, sizeof(int32_t) * (B > 0 ? B : 1), stream>>>(
+        lens, ended, B, tables, width, free_blocks, n_free, free_count, log2_of(page), count_out);
+    return hipGetLastError();
+  });
 }
 
 }  // namespace rfq
