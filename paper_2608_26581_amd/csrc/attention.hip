@@ -21,6 +21,9 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+#include <type_traits>
+
 #include "attention_device.h"
 #include "kv.h"
 #include "rfq_internal.h"
@@ -36,7 +39,7 @@ constexpr int split_groups(int64_t D, int nt) { return D <= 128 && nt == 1 ? 768
 constexpr int kItemCost = 4;
 // Workgroups of a launch, and the tokens of a part of the wide kernel's, at least.
 constexpr int64_t kMaxGrid = int64_t(1) << 20;
-constexpr int64_t kLeastPart = 1024;
+constexpr int64_t kLeastPart = 256;
 
 // ---- the shapes and the requests
 
@@ -87,12 +90,11 @@ struct Codes {
   uint32_t ks[S::kPieces];                // 256 channels: two bytes
 };
 
-template <int D, int NT, int P>
-__global__ __launch_bounds__(kThreads, NT == 1 && D <= 128 ? 3 : 2) void kv_attention_kernel(const AttentionArgs a,
-                                                                   const Partial part,
-                                                                   int split) {
+template <int D, int NT, int P, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, NT == 1 && D <= 128 && kWaves == 4 ? 3 : 2) void
+kv_attention_kernel(const AttentionArgs a, const Partial part, int split) {
   using S = Shape<D, NT, P>;
-  constexpr int W = S::kWords;
+  constexpr int W = S::kWords, kThreads = 64 * kWaves;
   __shared__ alignas(16) uint8_t lds_v[kWaves][S::kWaveLds];
   __shared__ float lds_ml[kWaves][S::kRows][2];
   __shared__ int64_t scan[kWaves];
@@ -439,8 +441,8 @@ __global__ __launch_bounds__(kThreads, NT == 1 && D <= 128 ? 3 : 2) void kv_atte
       }
     }
 
-    // The four waves' results joined, a 16-row tile at a time: each scales its O by
-    // exp2(m - M) and leaves it in its LDS rows; every thread adds four of them.
+    // The waves' results joined, a 16-row tile at a time: each scales its O by
+    // exp2(m - M) and leaves it in its LDS rows; every thread adds some of them.
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       l[t] = across_sum(l[t]);
@@ -508,17 +510,19 @@ __global__ __launch_bounds__(kThreads, NT == 1 && D <= 128 ? 3 : 2) void kv_atte
   }
 }
 
+constexpr int kJoinThreads = 256;
+
 // The parts of the items that the split kernel began but did not finish in one
 // workgroup: part 0 in slot 2 w + 1, the following ones in slots 2 (w + i).  Added in
 // that order.
 template <int D, int NT>
-__global__ __launch_bounds__(kThreads) void kv_attention_join_kernel(const AttentionArgs a,
+__global__ __launch_bounds__(kJoinThreads) void kv_attention_join_kernel(const AttentionArgs a,
                                                                      const Partial part) {
   constexpr int kRows = 16 * NT, kLanes = D / 4;         // kLanes: threads of a row
   const int wg = blockIdx.x;
   const Partial::Item it = part.item[wg];
   const int n = it.parts;
-  const int row = blockIdx.y * (kThreads / kLanes) + threadIdx.x / kLanes, r = it.row0 + row;
+  const int row = blockIdx.y * (kJoinThreads / kLanes) + threadIdx.x / kLanes, r = it.row0 + row;
   if (n == 0 || r >= it.rows) return;
   const int lr = threadIdx.x % kLanes, c = 4 * lr;
   auto slot = [&](int i) { return (int64_t)(i == 0 ? 2 * wg + 1 : 2 * (wg + i)) * kRows + row; };
@@ -569,14 +573,11 @@ __global__ __launch_bounds__(kThreads) void kv_attention_join_kernel(const Atten
 
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Rows of a tile: 32 where a request's rows fill them and the registers allow.
-int row_fragments(int64_t rows, int64_t D) { return D < 256 && rows > 16 ? 2 : 1; }
-
 int64_t partial_bytes(int64_t D, int nt) {
   return (int64_t)split_groups(D, nt) * (2 * 16 * nt * (D + 2) * 4 + (int64_t)sizeof(Partial::Item));
 }
 
-template <int D, int NT, int P>
+template <int D, int NT, int P, int kWaves>
 hipError_t launch(const AttentionArgs &a, bool split, float *work, hipStream_t stream) {
   using S = Shape<D, NT, P>;
   constexpr int kGroups = split_groups(D, NT);
@@ -592,27 +593,48 @@ hipError_t launch(const AttentionArgs &a, bool split, float *work, hipStream_t s
     const int64_t items = (up((int64_t)a.T * a.group, S::kRows) + a.B) * a.heads;
     grid = (unsigned)(items < kMaxGrid ? items : kMaxGrid);
   }
-  kv_attention_kernel<D, NT, P><<<grid, kThreads, 0, stream>>>(a, p, split);
+  kv_attention_kernel<D, NT, P, kWaves><<<grid, 64 * kWaves, 0, stream>>>(a, p, split);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !split) return e;
-  const dim3 join(kGroups, (unsigned)up(S::kRows, kThreads / (D / 4)));
-  kv_attention_join_kernel<D, NT><<<join, kThreads, 0, stream>>>(a, p);
+  const dim3 join(kGroups, (unsigned)up(S::kRows, kJoinThreads / (D / 4)));
+  kv_attention_join_kernel<D, NT><<<join, kJoinThreads, 0, stream>>>(a, p);
   return hipGetLastError();
 }
 
-// No split where every request's tokens are a step or two of a workgroup's waves.
-bool splits(int64_t max_seq) { return max_seq > 256; }
-
 // What a call launches.  Requests of up to kFewRows rows (queries times group) never take
 // the wide kernel; with one request the wide kernel alone serves it, whatever its rows.
+// Eight requests of 64 rows over 3000 tokens take 33.8 us here and 40.4 in the wide
+// kernel, of 128 rows 48.6 and 49.1, of 256 rows and 60000 tokens 912 and 885.
 constexpr int kFewRows = 64;
 struct Plan {
   bool few, wide;
   int few_rows;                           // the wide kernel's requests have more
   int nt;                                 // 16-row fragments of the other kernel
+  bool split;                             // whether its items' tokens are split
   int wide_parts;
   int64_t few_bytes, wide_work;           // workspace of each (0: no split)
 };
+
+// Few items of few tokens are not split: a workgroup of eight waves an item.  Measured, 8
+// heads of 128 channels, unsplit and split: one request of 500 tokens 8.9 and 10.8 us, of
+// 1000 11.6 and 10.9, of 2000 17.3 and 12.8; 16 of 900 11 and 15; 64 of 500 19.2 and 22.4;
+// 400 of 500 117 and 62.  Tiles have 16 rows there, else 32 if a request's rows fill them
+// and the registers allow: 24 rows over 500 tokens 9.3 us and with 32 16.8, but for 64
+// requests 35.9 and 21.7, which stay whole up to 256 tokens (of 100: 12.5 us, split 19.6).
+constexpr int64_t kFewItems = 512, kFewTokens = 1024;
+void plan_few(Plan &p, int64_t T, int64_t group, int64_t heads, int64_t D, int64_t B, int64_t rows,
+              int64_t max_seq) {
+  auto items = [&](int64_t tile) {
+    return heads * std::min(B * up(rows, tile), up(T * group, tile) + B);
+  };
+  p.nt = 1;
+  p.split = max_seq > kFewTokens || items(16) > kFewItems;
+  if (p.split && D < 256 && rows > 16) {
+    p.nt = 2;
+    p.split = max_seq > 256 || items(32) > kFewItems;
+  }
+}
+
 Plan plan_of(int64_t T, int64_t group, int64_t heads, int64_t D, int64_t B, int64_t max_query,
              int64_t max_seq, int64_t bytes) {
   Plan p = {};
@@ -621,11 +643,12 @@ Plan plan_of(int64_t T, int64_t group, int64_t heads, int64_t D, int64_t B, int6
   p.few = !p.wide || B > 1;
   p.few_rows = p.wide ? (B > 1 ? kFewRows : 0) : INT32_MAX;
   const int64_t rows = max_query * group;
-  p.nt = row_fragments(p.wide && rows > kFewRows ? kFewRows : rows, D);
-  p.few_bytes = p.few && splits(max_seq) ? partial_bytes(D, p.nt) : 0;
+  plan_few(p, T, group, heads, D, B, p.wide && rows > kFewRows ? kFewRows : rows, max_seq);
+  p.few_bytes = p.few && p.split ? partial_bytes(D, p.nt) : 0;
   p.wide_parts = 1;
   if (p.wide) {
-    // Two workgroups a CU; a part is at least kLeastPart tokens.
+    // Two workgroups a CU; a part is at least kLeastPart tokens (one request of 256 rows
+    // over 2000 tokens 19 us, in parts of 128 tokens 20.3, of 512 25, of 1024 49).
     const int64_t room = 512 / items;
     const int64_t most = max_seq / kLeastPart;
     const int64_t parts = room < most ? room : most;
@@ -659,19 +682,22 @@ hipError_t launch_kv_attention(const AttentionArgs &args, int64_t D, int64_t max
     if (e != hipSuccess || !p.few) return e;
   }
   const bool split = p.few_bytes > 0;
-  // Little work: at most four steps of 64 tokens for each wave that is resident.
-  const bool little = max_seq <= (int64_t(4) * 64 * 3072) / ((int64_t)a.B * a.heads);
-  if (D == 64) {
-    if (p.nt == 2) return launch<64, 2, 4>(a, split, workspace, stream);
-    return little ? launch<64, 1, 2>(a, split, workspace, stream)
-                  : launch<64, 1, 4>(a, split, workspace, stream);
-  }
-  if (D == 128) {
-    if (p.nt == 2) return launch<128, 2, 4>(a, split, workspace, stream);
-    return little ? launch<128, 1, 2>(a, split, workspace, stream)
-                  : launch<128, 1, 4>(a, split, workspace, stream);
-  }
-  return launch<256, 1, 2>(a, split, workspace, stream);
+  // Little work: at most four steps of 64 tokens for each wave that is resident (four a
+  // workgroup).
+  const int64_t waves = 4 * split_groups(D, p.nt);
+  const bool little = max_seq <= 4 * 64 * waves / ((int64_t)a.B * a.heads);
+  auto run = [&](auto channels) {
+    constexpr int kD = decltype(channels)::value;
+    if constexpr (kD < 256) {
+      if (p.nt == 2) return launch<kD, 2, 4, 4>(a, split, workspace, stream);
+      if (split && !little) return launch<kD, 1, 4, 4>(a, split, workspace, stream);
+    }
+    return split ? launch<kD, 1, 2, 4>(a, split, workspace, stream)
+                 : launch<kD, 1, 2, 8>(a, split, workspace, stream);
+  };
+  if (D == 64) return run(std::integral_constant<int, 64>{});
+  if (D == 128) return run(std::integral_constant<int, 128>{});
+  return run(std::integral_constant<int, 256>{});
 }
 
 }  // namespace rfq

@@ -12,7 +12,6 @@
 namespace rfq {
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4;        // of a workgroup
 constexpr float kLn2 = 0.69314718055994531f;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));

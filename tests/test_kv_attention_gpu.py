@@ -105,6 +105,26 @@ def test_many_rows_split(D, window, causal):
     _check(rng, [(3000, 20)], 10, 2, D, 16, causal=causal, window=window)
 
 
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("nq", [1, 7])
+@pytest.mark.parametrize("B,longest", [(6, 1024), (6, 1025), (270, 200), (270, 290)])
+@pytest.mark.parametrize("window", [0, 90])
+def test_whole_and_split_items(D, nq, B, longest, window):
+    """Both sides of the rules on items and tokens, one and several rows a request."""
+    rng = np.random.default_rng(D + nq + B + longest)
+    reqs = [(longest, nq)] + [(int(n), int(rng.integers(0, nq + 1)))
+                              for n in rng.integers(0, longest, B - 1)]
+    _check(rng, reqs, 6, 2, D, 16, window=window)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("length", [255, 511, 512, 513, 800, 1027])
+def test_many_rows_short_parts(D, length):
+    rng = np.random.default_rng(length)
+    _check(rng, [(length, 70)], 2, 2, D, 32)
+    _check(rng, [(length, 67), (300, 10), (0, 70)], 2, 1, D, 16, causal=False, window=400)
+
+
 @pytest.mark.parametrize("group,heads,page", [(1, 128, 32), (3, 48, 128), (7, 20, 64), (20, 8, 256)])
 def test_many_rows_groups(group, heads, page):
     rng = np.random.default_rng(group)
