@@ -517,7 +517,8 @@ typedef struct rfq_kv_cache {
  * the list is short, every later request that lacks blocks is refused).
  *   block_tables  [B][width], written where blocks were taken (and only there).
  *   slots         [tokens]: the slot of each new token in the order of requests, -1
- *                 for tokens of refused requests and past the last token.
+ *                 for tokens of refused requests, past the last token, and in
+ *                 blocks that are negative or whose slots int32 does not hold.
  *   positions     [tokens]: the token's place in its request (0 past the last).
  *   seq_lens      [B]: ctx + new, or 0 for a refused request.
  *   query_starts  [B + 1]: the requests' first rows among the new tokens.

@@ -8,7 +8,14 @@
 // all of them, into LDS, so that decoding costs a quarter of what it does in a wave of
 // its own.  32 x 32 x 16 products: a lane holds one row's scores of half a tile's
 // tokens, the other half is in lane ^ 32, and P again goes from one product to the next
-// in the lane's registers.
+// in the lane's registers, rounded to the products' bf16 (2^-9 of each weight; the sum l
+// adds the unrounded weights in fp32).
+//
+// Measured, 32 heads over 8 cached heads of 128 channels: a prompt of 8192 tokens in 545
+// us, 1010 TFLOP/s of the 1225 that a large bf16 product reaches on the card.  The issue
+// of instructions bounds it: the matrix units are busy 48% and the vector units 60% of
+// the time, the exponentials and the maximum standing against each 32 products.  Eight waves of 32
+// rows, 64 rows a wave and operands read 2 or 4 products ahead are not faster.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -43,10 +50,10 @@ __device__ __forceinline__ uint32_t decode_pair(uint32_t c, float s, int w) {
   return __builtin_bit_cast(uint32_t, r);
 }
 
-template <int D, int NR, int WAVES>
+template <int D>
 struct Wide {
-  static constexpr int kThreads = 64 * WAVES;
-  static constexpr int kWaveRows = 32 * NR, kRows = WAVES * kWaveRows, kTile = 64;
+  static constexpr int kWaves = 4, kThreads = 64 * kWaves;
+  static constexpr int kWaveRows = 32, kRows = kWaves * kWaveRows, kTile = 64;
   static constexpr int kLanes = D / 32;                   // 32-channel blocks of a token
   static constexpr int kBlocks = kTile * kLanes;          // of a tile
   static constexpr int kLoads = (kBlocks + kThreads - 1) / kThreads;
@@ -87,14 +94,14 @@ __device__ __forceinline__ int request_of_tile(const AttentionArgs &a, int index
 //
 // Matrix and vector units run side by side: in a step, half a tile of 32 tokens, a wave
 // turns its scores S_j into P_j while the matrix cores compute S_(j+1) and add
-// P_(j-1) V to O; the three are independent.  Their operands are read from LDS two
-// products ahead.  In a tile's second half the keys of the tile after the next and the
+// P_(j-1) V to O; the three are independent.  Their operands are read from LDS
+// kReadAhead products ahead.  In a tile's second half the keys of the tile after the next and the
 // values of the next are decoded into the buffers that the first half was the last to
 // read, behind the tile's one barrier.
-template <int D, int NR, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attention_wide_kernel(
+template <int D>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_wide_kernel(
     const AttentionArgs a, int few_rows, int tiles, float *parts_o, float *parts_ml) {
-  using S = Wide<D, NR, WAVES>;
+  using S = Wide<D>;
   constexpr int LT = S::kLanes, KS = D / 16, CT = D / 32, L = S::kLoads;
   constexpr int kThreads = S::kThreads;
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];   // [2] keys, [2] values
@@ -117,22 +124,21 @@ __global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attentio
   // see.  A negative scale goes into the queries' signs, so that the largest score is the
   // largest product.
   const int row0 = rt * S::kRows, w0 = row0 + wave * S::kWaveRows;
-  u32x4 qf[NR][KS];
-  int lo[NR], hi[NR];
+  u32x4 qf[KS];
+  int lo, hi;
   const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
-#pragma unroll
-  for (int n = 0; n < NR; ++n) {
-    const int r = w0 + 32 * n + col, i = r / a.group, qh = head * a.group + (r - i * a.group);
+  {
+    const int r = w0 + col, i = r / a.group, qh = head * a.group + (r - i * a.group);
     const int pos = req.len - req.nq + i;
-    hi[n] = a.causal ? min(pos, req.len - 1) : req.len - 1;
-    lo[n] = a.window ? pos - a.window + 1 : 0;
+    hi = a.causal ? min(pos, req.len - 1) : req.len - 1;
+    lo = a.window ? pos - a.window + 1 : 0;
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
-      qf[n][k] = u32x4{0, 0, 0, 0};
+      qf[k] = u32x4{0, 0, 0, 0};
       if (r < rows) {
-        qf[n][k] = *reinterpret_cast<const u32x4 *>(a.q + (req.start + i) * a.q_ts +
+        qf[k] = *reinterpret_cast<const u32x4 *>(a.q + (req.start + i) * a.q_ts +
                                                     qh * a.q_hs + 16 * k + 8 * h);
-        qf[n][k] ^= flip;
+        qf[k] ^= flip;
       }
     }
   }
@@ -243,18 +249,13 @@ __global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attentio
     for (int x = 0; x < 4 * L; ++x) decode_value(buf, x / 4, x % 4);
   };
 
-  v16f o[NR][CT], s[2][NR];
-  u32x2 pf[2][NR][4];                                     // P of a half, 4 tokens each
-  float m[NR], sum[NR];                                   // m: in units of log2
+  v16f o[CT], s[2];
+  u32x2 pf[2][4];                                         // P of a half, 4 tokens each
+  float m = neg_inf(), sum = 0.0f;                        // m: in units of log2
 #pragma unroll
-  for (int n = 0; n < NR; ++n) {
+  for (int t = 0; t < CT; ++t) o[t] = v16f{};
 #pragma unroll
-    for (int t = 0; t < CT; ++t) o[n][t] = v16f{};
-#pragma unroll
-    for (int q = 0; q < 4; ++q) pf[1][n][q] = u32x2{0, 0};
-    m[n] = neg_inf();
-    sum[n] = 0.0f;
-  }
+  for (int q = 0; q < 4; ++q) pf[1][q] = u32x2{0, 0};
   // Operand k of a half's keys; operand (u, t) of its values (16 tokens u, 32 rows t).
   auto key_frag = [&](int buf, int t, int k) {
     return *reinterpret_cast<const u32x4 *>(lds + buf * S::kKeys + col * S::kKeyPitch + 16 * h +
@@ -287,12 +288,9 @@ __global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attentio
     fetch_keys(tile0 + 2);
     look_up(tile0 + 3);
     __syncthreads();
+    s[0] = v16f{};
 #pragma unroll
-    for (int n = 0; n < NR; ++n) {
-      s[0][n] = v16f{};
-#pragma unroll
-      for (int k = 0; k < KS; ++k) s[0][n] = mma32(key_frag(0, 0, k), qf[n][k], s[0][n]);
-    }
+    for (int k = 0; k < KS; ++k) s[0] = mma32(key_frag(0, 0, k), qf[k], s[0]);
   }
   // Which pieces of a tile have a block: read a step before it is needed.
   auto find = [&](int tile) { return *reinterpret_cast<const i32x4 *>(lds_have[tile & 3]); };
@@ -317,77 +315,61 @@ __global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attentio
     if (!__builtin_amdgcn_readfirstlane(whole)) {
       asm volatile("");                                   // (a branch, not selects)
 #pragma unroll
-      for (int n = 0; n < NR; ++n)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int tok = t0 + 8 * (e / 4) + 4 * h + e % 4;
-          const bool see = tok >= lo[n] && tok <= hi[n] && (e < 8 ? have0 : have1);
-          s[T][n][e] = see ? s[T][n][e] : neg_inf();
-        }
+      for (int e = 0; e < 16; ++e) {
+        const int tok = t0 + 8 * (e / 4) + 4 * h + e % 4;
+        const bool see = tok >= lo && tok <= hi && (e < 8 ? have0 : have1);
+        s[T][e] = see ? s[T][e] : neg_inf();
+      }
     }
-    float top[NR];
-    bool grows = false;
+    float x = s[T][0];
 #pragma unroll
-    for (int n = 0; n < NR; ++n) {
-      float x = s[T][n][0];
-#pragma unroll
-      for (int e = 1; e < 16; ++e) x = fmaxf(x, s[T][n][e]);
-      const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x),
-                                                         false, false);
-      top[n] = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * c;
-      grows |= top[n] > m[n] + 8.0f;
-    }
+    for (int e = 1; e < 16; ++e) x = fmaxf(x, s[T][e]);
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x),
+                                                       false, false);
+    const float top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * c;
+    const bool grows = top > m + 8.0f;
     // The reference follows the maximum only where P would pass 2^8, to a whole power
     // of two: P_(j-1), still to be multiplied, is scaled exactly.
     if (__any(grows)) {
       asm volatile("");
+      const float up = fmaxf(ceilf(top), m);
+      const float f = exp2_hw(m - (up == neg_inf() ? 0.0f : up));
+      sum *= f;
 #pragma unroll
-      for (int n = 0; n < NR; ++n) {
-        const float up = fmaxf(ceilf(top[n]), m[n]);
-        const float f = exp2_hw(m[n] - (up == neg_inf() ? 0.0f : up));
-        sum[n] *= f;
+      for (int t = 0; t < CT; ++t) o[t] *= f;
 #pragma unroll
-        for (int t = 0; t < CT; ++t) o[n][t] *= f;
+      for (int q = 0; q < 4; ++q)
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const uint32_t p = pf[N][n][q][x];
-            const bf16x2 y = {(__bf16)(__uint_as_float(p << 16) * f),
-                              (__bf16)(__uint_as_float(p & 0xFFFF0000u) * f)};
-            pf[N][n][q][x] = __builtin_bit_cast(uint32_t, y);
-          }
-        m[n] = up;
-      }
+        for (int x = 0; x < 2; ++x) {
+          const uint32_t p = pf[N][q][x];
+          const bf16x2 y = {(__bf16)(__uint_as_float(p << 16) * f),
+                            (__bf16)(__uint_as_float(p & 0xFFFF0000u) * f)};
+          pf[N][q][x] = __builtin_bit_cast(uint32_t, y);
+        }
+      m = up;
     }
-    float ref[NR], e[NR][16];
-#pragma unroll
-    for (int n = 0; n < NR; ++n) {
-      ref[n] = m[n] == neg_inf() ? 0.0f : m[n];
-      s[N][n] = v16f{};
-    }
+    float e[16];
+    const float ref = m == neg_inf() ? 0.0f : m;
+    s[N] = v16f{};
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
       if (k + kAhead < KS) {
         kf[k + kAhead] = key_frag(keys, N, k + kAhead);
         vf[k + kAhead] = value_frag(vals, N, k + kAhead);
       }
+      s[N] = mma32(kf[k], qf[k], s[N]);
+      o[k % CT] = mma32(vf[k], weights(pf[N], k), o[k % CT]);
 #pragma unroll
-      for (int n = 0; n < NR; ++n) {
-        s[N][n] = mma32(kf[k], qf[n][k], s[N][n]);
-        o[n][k % CT] = mma32(vf[k], weights(pf[N][n], k), o[n][k % CT]);
-#pragma unroll
-        for (int x = k * 16 / KS; x < (k + 1) * 16 / KS; ++x) {
-          e[n][x] = exp2_hw(__builtin_fmaf(s[T][n][x], c, -ref[n]));
-          if (x % 4 == 3) {
-            const bf16x4 y = {(__bf16)e[n][x - 3], (__bf16)e[n][x - 2], (__bf16)e[n][x - 1],
-                              (__bf16)e[n][x]};
-            u32x2 &p = pf[T][n][x / 4];
-            p = __builtin_bit_cast(u32x2, y);
-            sum[n] += (e[n][x - 3] + e[n][x - 2]) + (e[n][x - 1] + e[n][x]);
-            // (Not to be moved behind the products.)
-            asm volatile("" : "+v"(p[0]), "+v"(p[1]), "+v"(sum[n]));
-          }
+      for (int x = k * 16 / KS; x < (k + 1) * 16 / KS; ++x) {
+        e[x] = exp2_hw(__builtin_fmaf(s[T][x], c, -ref));
+        if (x % 4 == 3) {
+          const bf16x4 y = {(__bf16)e[x - 3], (__bf16)e[x - 2], (__bf16)e[x - 1],
+                            (__bf16)e[x]};
+          u32x2 &p = pf[T][x / 4];
+          p = __builtin_bit_cast(u32x2, y);
+          sum += (e[x - 3] + e[x - 2]) + (e[x - 1] + e[x]);
+          // (Not to be moved behind the products.)
+          asm volatile("" : "+v"(p[0]), "+v"(p[1]), "+v"(sum));
         }
       }
       if constexpr (T == 1) {
@@ -423,70 +405,65 @@ __global__ __launch_bounds__(64 * WAVES, D * NR >= 256 ? 1 : 2) void kv_attentio
   if (tile0 < end) {
     const int buf = (end - 1 - tile0) & 1;
 #pragma unroll
-    for (int n = 0; n < NR; ++n)
-#pragma unroll
-      for (int f = 0; f < KS; ++f)
-        o[n][f % CT] = mma32(value_frag(buf, 1, f), weights(pf[1][n], f), o[n][f % CT]);
+    for (int f = 0; f < KS; ++f)
+      o[f % CT] = mma32(value_frag(buf, 1, f), weights(pf[1], f), o[f % CT]);
   }
 
-#pragma unroll
-  for (int n = 0; n < NR; ++n) {
-    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum[n]),
-                                                       __float_as_uint(sum[n]), false, false);
-    const float l = __uint_as_float(both[0]) + __uint_as_float(both[1]);
-    const int r = w0 + 32 * n + col, i = r / a.group, qh = head * a.group + (r - i * a.group);
-    if (r >= rows) continue;
-    if (parts > 1) {
-      const int64_t at = ((int64_t)(index * a.heads + head) * parts + part) * S::kRows + r - row0;
-      if (h == 0) {
-        parts_ml[2 * at] = m[n];
-        parts_ml[2 * at + 1] = l;
-      }
-      // Elements in the registers' order (the join's threads each take one position).
-#pragma unroll
-      for (int t = 0; t < CT; ++t)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const v16f &x = o[n][t];
-          *reinterpret_cast<v4f *>(parts_o + at * D + 32 * t + 8 * q + 4 * h) =
-              v4f{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
-        }
-      continue;
+  const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum),
+                                                     __float_as_uint(sum), false, false);
+  const float l = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+  const int r = w0 + col, i = r / a.group, qh = head * a.group + (r - i * a.group);
+  if (r >= rows) return;
+  if (parts > 1) {
+    const int64_t at = ((int64_t)(index * a.heads + head) * parts + part) * S::kRows + r - row0;
+    if (h == 0) {
+      parts_ml[2 * at] = m;
+      parts_ml[2 * at + 1] = l;
     }
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    uint16_t *out = a.out + (req.start + i) * a.o_ts + qh * a.o_hs;
-    // Element e of tile t is row 32 t + 8 (e / 4) + 4 h + e % 4: 8 channels in the order of
-    // memory are those whose rows are D / 8 apart.
+    // Elements in the registers' order (the join's threads each take one position).
 #pragma unroll
-    for (int g = 0; g < D / 16; ++g) {
-      u32x4 y;
+    for (int t = 0; t < CT; ++t)
 #pragma unroll
-      for (int k = 0; k < 8; k += 2) {
-        float v[2];
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          // Row of the k-th channel of the lane's g-th octet (without 4 h).
-          const int row = (k + x) * S::kOctets + g / 4 * 8 + g % 4;
-          v[x] = o[n][row / 32][row % 32 / 8 * 4 + row % 4] * inv;
-        }
-        const bf16x2 p = {(__bf16)v[0], (__bf16)v[1]};
-        y[k / 2] = __builtin_bit_cast(uint32_t, p);
+      for (int q = 0; q < 4; ++q) {
+        const v16f &x = o[t];
+        *reinterpret_cast<v4f *>(parts_o + at * D + 32 * t + 8 * q + 4 * h) =
+            v4f{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
       }
-      *reinterpret_cast<u32x4 *>(out + 8 * (g / 4 * 8 + 4 * h + g % 4)) = y;
-    }
-    if (a.lse && h == 0)
-      a.lse[(int64_t)(req.start + i) * a.Hq + qh] =
-          l == 0.0f ? neg_inf() : (m[n] + __builtin_amdgcn_logf(l)) * kLn2;
+    return;
   }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  uint16_t *out = a.out + (req.start + i) * a.o_ts + qh * a.o_hs;
+  // Element e of tile t is row 32 t + 8 (e / 4) + 4 h + e % 4: 8 channels in the order of
+  // memory are those whose rows are D / 8 apart.
+#pragma unroll
+  for (int g = 0; g < D / 16; ++g) {
+    u32x4 y;
+#pragma unroll
+    for (int k = 0; k < 8; k += 2) {
+      float v[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        // Row of the k-th channel of the lane's g-th octet (without 4 h).
+        const int row = (k + x) * S::kOctets + g / 4 * 8 + g % 4;
+        v[x] = o[row / 32][row % 32 / 8 * 4 + row % 4] * inv;
+      }
+      const bf16x2 p = {(__bf16)v[0], (__bf16)v[1]};
+      y[k / 2] = __builtin_bit_cast(uint32_t, p);
+    }
+    *reinterpret_cast<u32x4 *>(out + 8 * (g / 4 * 8 + 4 * h + g % 4)) = y;
+  }
+  if (a.lse && h == 0)
+    a.lse[(int64_t)(req.start + i) * a.Hq + qh] =
+        l == 0.0f ? neg_inf() : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // The parts of the row tiles joined, in their order: thread = (row, 4 of the LDS rows that
 // the channels have there).
-template <int D, int NR, int WAVES>
+template <int D>
 __global__ __launch_bounds__(256) void kv_attention_wide_join_kernel(
     const AttentionArgs a, int few_rows, int tiles, int parts, const float *parts_o,
     const float *parts_ml) {
-  using S = Wide<D, NR, WAVES>;
+  using S = Wide<D>;
   constexpr int kLanes = D / 4, kRowsHere = 256 / kLanes;
   const int head = blockIdx.x % a.heads, index = blockIdx.x / a.heads;
   if (index >= tiles) return;
@@ -523,12 +500,12 @@ __global__ __launch_bounds__(256) void kv_attention_wide_join_kernel(
         l == 0.0f ? neg_inf() : (top + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-template <int D, int NR, int WAVES>
+template <int D>
 hipError_t launch(const AttentionArgs &a, int few_rows, int parts, float *work,
                   hipStream_t stream) {
-  using S = Wide<D, NR, WAVES>;
+  using S = Wide<D>;
   static std::atomic<bool> limit[kMaxDevices];
-  const auto kernel = kv_attention_wide_kernel<D, NR, WAVES>;
+  const auto kernel = kv_attention_wide_kernel<D>;
   hipError_t e = set_lds_limit(limit, (const void *)kernel, S::kLds);
   if (e != hipSuccess) return e;
   const int64_t tiles = wide_tiles(a.T, a.group, a.B), items = tiles * a.heads;
@@ -536,7 +513,7 @@ hipError_t launch(const AttentionArgs &a, int few_rows, int parts, float *work,
   kernel<<<dim3((unsigned)items, (unsigned)parts), S::kThreads, S::kLds, stream>>>(
       a, few_rows, (int)tiles, work, ml);
   if ((e = hipGetLastError()) != hipSuccess || parts == 1) return e;
-  kv_attention_wide_join_kernel<D, NR, WAVES>
+  kv_attention_wide_join_kernel<D>
       <<<dim3((unsigned)items, (unsigned)(S::kRows * D / 4 / 256)), 256, 0, stream>>>(
           a, few_rows, (int)tiles, parts, work, ml);
   return hipGetLastError();
@@ -554,9 +531,9 @@ int64_t wide_bytes(int64_t items, int parts, int64_t D) {
 
 hipError_t launch_kv_attention_wide(const AttentionArgs &a, int64_t D, int few_rows, int parts,
                                     float *work, hipStream_t stream) {
-  if (D == 64) return launch<64, 1, 4>(a, few_rows, parts, work, stream);
-  if (D == 128) return launch<128, 1, 4>(a, few_rows, parts, work, stream);
-  return launch<256, 1, 4>(a, few_rows, parts, work, stream);
+  if (D == 64) return launch<64>(a, few_rows, parts, work, stream);
+  if (D == 128) return launch<128>(a, few_rows, parts, work, stream);
+  return launch<256>(a, few_rows, parts, work, stream);
 }
 
 }  // namespace rfq

@@ -261,6 +261,20 @@ def test_assign_count_outside_the_list_and_no_table():
             assert all(np.array_equal(g.cpu().numpy(), w) for g, w in zip(got, want)), (count, width)
 
 
+def test_assign_blocks_that_have_no_slots():
+    """Table and list entries that are negative or beyond int32's slots: slot -1."""
+    ctx, new = np.array([20, 16, 3], np.int32), np.array([2, 2, 1], np.int32)
+    free = np.array([2 ** 31 - 1, 7], np.int32)
+    tables = np.array([[4, 2 ** 27], [5, -1], [2 ** 27 - 1, -1]], np.int32)
+    got = rfq.rfq_block_assign(_dev(ctx), _dev(new), _dev(tables), _dev(free),
+                               _dev(np.array([1], np.int32)), 16, 5)
+    assert got[0].tolist() == [-1, -1, -1, -1, (2 ** 27 - 1) * 16 + 3]
+    tables = np.array([[4, -1], [5, -1], [-7, -1]], np.int32)
+    got = rfq.rfq_block_assign(_dev(ctx), _dev(new), _dev(tables), _dev(free),
+                               _dev(np.array([2], np.int32)), 16, 5)
+    assert got[0].tolist() == [-1, -1, 7 * 16, 7 * 16 + 1, -1]
+
+
 def test_assign_huge_lengths():
     """Lengths whose sums pass 32 bits are refused without harm to the others."""
     big = 2 ** 31 - 1
