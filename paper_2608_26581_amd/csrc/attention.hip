@@ -43,8 +43,13 @@ namespace rfq {
 namespace {
 
 // Workgroups that the split kernel's work is divided over: three per CU where the
-// registers allow three waves a SIMD, else two.
-constexpr int split_groups(int64_t D, int nt) { return D <= 128 && nt == 1 ? 768 : 512; }
+// registers allow three waves a SIMD, else two.  64 channels allow four, which long work
+// takes (requests' heads times tokens): 4 requests of 131072 tokens and 8 heads 78.3 us, with
+// three 85.5, but 64 requests of 2000 29.3 and 28.6.
+constexpr int split_groups(int64_t D, int nt, int64_t heads, int64_t tokens) {
+  if (nt == 2 || D == 256) return 512;
+  return D == 64 && tokens >= (int64_t(1) << 21) / heads ? 1024 : 768;
+}
 // An item's queries, its first loads and the joining of the waves take about as long
 // as this many tiles.
 constexpr int kItemCost = 4;
@@ -106,7 +111,7 @@ struct Codes {
 };
 
 template <int D, int NT, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, NT == 1 && D <= 128 && kWaves == 4 ? 3 : 2) void
+__global__ __launch_bounds__(64 * kWaves, NT == 1 && D <= 128 && kWaves == 4 ? (D == 64 ? 4 : 3) : 2) void
 kv_attention_kernel(const AttentionArgs a, const Partial part, int split) {
   // Steps of 32 tokens, of 64, or what the work asks for.
   constexpr bool kShort = NT == 1, kLong = D < 256 && kWaves == 4;
@@ -603,22 +608,21 @@ __global__ __launch_bounds__(kJoinThreads) void kv_attention_join_kernel(const A
 
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-int64_t partial_bytes(int64_t D, int nt) {
-  return (int64_t)split_groups(D, nt) *
-         (2 * 16 * nt * (D + 2) * 4 + (int64_t)sizeof(Partial::Item));
+int64_t partial_bytes(int64_t D, int nt, int64_t groups) {
+  return groups * (2 * 16 * nt * (D + 2) * 4 + (int64_t)sizeof(Partial::Item));
 }
 
 template <int D, int NT, int kWaves>
-hipError_t launch(const AttentionArgs &a, bool split, float *work, hipStream_t stream) {
+hipError_t launch(const AttentionArgs &a, unsigned groups, float *work, hipStream_t stream) {
   using S = Shape<D, NT, 4>;
-  constexpr int kGroups = split_groups(D, NT);
+  const bool split = groups > 0;
   Partial p = {};
   unsigned grid;
   if (split) {
     p.o = work;
-    p.ml = work + (int64_t)kGroups * 2 * S::kRows * D;
-    p.item = reinterpret_cast<Partial::Item *>(p.ml + (int64_t)kGroups * 2 * S::kRows * 2);
-    grid = kGroups;
+    p.ml = work + (int64_t)groups * 2 * S::kRows * D;
+    p.item = reinterpret_cast<Partial::Item *>(p.ml + (int64_t)groups * 2 * S::kRows * 2);
+    grid = groups;
   } else {
     // At least as many workgroups as there are items, within a launch's limits.
     const int64_t items = (up((int64_t)a.T * a.group, S::kRows) + a.B) * a.heads;
@@ -627,7 +631,7 @@ hipError_t launch(const AttentionArgs &a, bool split, float *work, hipStream_t s
   kv_attention_kernel<D, NT, kWaves><<<grid, 64 * kWaves, 0, stream>>>(a, p, split);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !split) return e;
-  const dim3 join(kGroups, (unsigned)up(S::kRows, kJoinThreads / (D / 4)));
+  const dim3 join(groups, (unsigned)up(S::kRows, kJoinThreads / (D / 4)));
   kv_attention_join_kernel<D, NT><<<join, kJoinThreads, 0, stream>>>(a, p);
   return hipGetLastError();
 }
@@ -644,6 +648,7 @@ struct Plan {
   int few_rows;                           // the wide kernel's requests have more
   int nt;                                 // 16-row fragments of the other kernel
   bool split;                             // whether its items' tokens are split
+  int groups;                             // into as many workgroups
   int wide_parts;
   int64_t few_bytes, wide_work;           // workspace of each (0: no split)
 };
@@ -677,7 +682,8 @@ Plan plan_of(int64_t T, int64_t group, int64_t heads, int64_t D, int64_t B, int6
   p.few_rows = p.few ? (p.wide ? kFewRows : INT32_MAX) : 0;
   const int64_t rows = max_query * group;
   plan_few(p, T, group, heads, D, B, p.wide && rows > kFewRows ? kFewRows : rows, max_seq);
-  p.few_bytes = p.few && p.split ? partial_bytes(D, p.nt) : 0;
+  p.groups = split_groups(D, p.nt, B * heads, max_seq);
+  p.few_bytes = p.few && p.split ? partial_bytes(D, p.nt, p.groups) : 0;
   p.wide_parts = 1;
   if (p.wide) {
     // Two workgroups a CU; a part is at least kLeastPart tokens (one request of 256 rows
@@ -714,13 +720,13 @@ hipError_t launch_kv_attention(const AttentionArgs &args, int64_t D, int64_t max
                                                   workspace + p.few_bytes / 4, stream);
     if (e != hipSuccess || !p.few) return e;
   }
-  const bool split = p.few_bytes > 0;
+  const unsigned groups = p.few_bytes > 0 ? p.groups : 0;        // (0: not split)
   auto run = [&](auto channels) {
     constexpr int kD = decltype(channels)::value;
     if constexpr (kD < 256)
-      if (p.nt == 2) return launch<kD, 2, 4>(a, split, workspace, stream);
-    return split ? launch<kD, 1, 4>(a, split, workspace, stream)
-                 : launch<kD, 1, 8>(a, split, workspace, stream);
+      if (p.nt == 2) return launch<kD, 2, 4>(a, groups, workspace, stream);
+    return groups ? launch<kD, 1, 4>(a, groups, workspace, stream)
+                  : launch<kD, 1, 8>(a, groups, workspace, stream);
   };
   if (D == 64) return run(std::integral_constant<int, 64>{});
   if (D == 128) return run(std::integral_constant<int, 128>{});

@@ -321,6 +321,23 @@ def test_workspace_and_bounds():
     ku.assert_attention_close(out.float().cpu().numpy(), lse.cpu().numpy(), ref)
 
 
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("reqs", [[(3000, 1), (0, 0), (700, 2)], [(900, 40), (2000, 1)]])
+@pytest.mark.parametrize("hint", [2 ** 21, 2 ** 62])
+def test_hints_beyond_the_lengths(D, reqs, hint):
+    """Upper bounds far above the lengths choose how the work is divided, nothing else."""
+    rng = np.random.default_rng(D)
+    lens = [n for n, _ in reqs]
+    cache = ku.Cache(rng, lens, 2, 16, D)
+    starts = _starts(reqs)
+    q = _queries(rng, int(starts[-1]), 8, D)
+    out, lse = rfq.rfq_kv_attention(
+        _dev(q.astype(np.float32)).bfloat16(), cache.device(), _dev(cache.tables),
+        _dev(np.array(lens, np.int32)), _dev(starts), 40, hint, return_lse=True)
+    ref = ku.attention(q, cache, lens, starts, D ** -0.5, True, 0)
+    ku.assert_attention_close(out.float().cpu().numpy(), lse.cpu().numpy(), ref, str(reqs))
+
+
 def test_same_bits_on_another_stream_and_in_a_graph():
     rng = np.random.default_rng(13)
     reqs = [(1500, 1), (40, 1), (700, 1)]
