@@ -591,7 +591,7 @@ rfq_status rfq_kv_gather(const rfq_kv_cache *cache, const int32_t *slots, int64_
 /*
  * Attention of the queries of B requests over their cached keys and values.
  * Request b holds the tokens 0 .. len - 1 (len = seq_lens[b], cut to [0, width *
- * page]), token j in block block_tables[b][j / page]; its queries are the rows
+ * page] and to 2^30), token j in block block_tables[b][j / page]; its queries are the rows
  * query_starts[b] .. query_starts[b + 1] - 1 of q, the last of them at token len - 1,
  * so row i of nq is at p = len - nq + i.  Row i attends to the tokens j with j < len,
  * with j <= p if causal is nonzero, and with j > p - window if window > 0:

@@ -676,6 +676,7 @@ void plan_few(Plan &p, int64_t T, int64_t group, int64_t heads, int64_t D, int64
 Plan plan_of(int64_t T, int64_t group, int64_t heads, int64_t D, int64_t B, int64_t max_query,
              int64_t max_seq, int64_t bytes) {
   Plan p = {};
+  max_query = std::min(max_query, T);     // (so that no product below passes 64 bits)
   const int64_t items = wide_tiles(T, group, B) * heads;
   p.wide = max_query * group > kFewRows && items > 0 && items <= kMaxGrid;
   p.few = !p.wide || (T - (B - 1) * max_query) * group <= kFewRows;

@@ -131,6 +131,17 @@ def test_attention_workspace():
         assert f(*bad) == 0, bad
 
 
+def test_attention_workspace_of_extreme_hints():
+    """No request has more queries than q has rows, whatever the hint says."""
+    f = binding.load().rfq_kv_attention_workspace_bytes
+    for sizes in ((64, 2 ** 24 - 1, 1, 64, 2 ** 23), (2 ** 23, 255, 255, 128, 2 ** 24 - 1),
+                  (2 ** 23, 255, 1, 256, 5), (700, 28, 4, 128, 2)):
+        for max_seq in (0, 4096, 2 ** 62):
+            want = f(*sizes, sizes[0], max_seq)
+            assert want >= 0
+            assert f(*sizes, 2 ** 31 - 1, max_seq) == want, (sizes, max_seq)
+
+
 def test_block_calls():
     call = _caller("rfq_block_assign", dict(
         ctx=A, new=A, B=-1, tables=A, width=4, free=A, n_free=9, count=A, page=16, tokens=4,
