@@ -26,9 +26,9 @@
 //
 // Measured, 8 cached heads of 128 channels, 32 of q: 4 requests of 131072 tokens in 119.5 us
 // and the join 6.5 (4.8 TB/s of the 5.1 that a large copy reaches on the card: bandwidth
-// bounds it); 64 requests of 1 to 8192 tokens, 54670 in all, 21.3 + 4.5 us (latency: a share is a few
-// steps of a wave); one of 700 tokens, whole items, 10.1 us (latency: the lookups, three
-// loads of codes one after another, and joining the waves).
+// bounds it); 64 requests of 1 to 8192 tokens, 54670 in all, 21.3 + 4.5 us (latency: a
+// share is a few steps of a wave); one of 700 tokens, whole items, 10.1 us (latency: the
+// lookups, three loads of codes one after another, and joining the waves).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -110,13 +110,20 @@ struct Codes {
   uint32_t ks[S::kPieces];                // 256 channels: two bytes
 };
 
+// Waves a SIMD that the registers have to allow (as split_groups counts on).
+constexpr int wave_bound(int D, int NT, int waves) {
+  if (NT == 2 || D == 256 || waves == 8) return 2;
+  return D == 64 ? 4 : 3;
+}
+
 template <int D, int NT, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, NT == 1 && D <= 128 && kWaves == 4 ? (D == 64 ? 4 : 3) : 2) void
-kv_attention_kernel(const AttentionArgs a, const Partial part, int split) {
+__global__ __launch_bounds__(64 * kWaves, wave_bound(D, NT, kWaves)) void kv_attention_kernel(
+    const AttentionArgs a, const Partial part, int split) {
   // Steps of 32 tokens, of 64, or what the work asks for.
   constexpr bool kShort = NT == 1, kLong = D < 256 && kWaves == 4;
   constexpr int kThreads = 64 * kWaves;
   using U = Shape<D, NT, 4>;              // (what is the same for both)
+  static_assert(U::kTile == kUnit, "requests are counted in units");
   __shared__ alignas(16) uint8_t lds_v[kWaves][U::kWaveLds];
   __shared__ float lds_ml[kWaves][U::kRows][2];
   __shared__ int64_t scan[kWaves];
