@@ -498,7 +498,8 @@ typedef struct rfq_rope_spec {
  * [blocks][heads][page][D / 32] of keys and of values, MXFP4 as above (blocks of
  * 32 channels).  Slot s is token s % page of block s / page.  All four pointers
  * are 16-byte aligned; the struct is in host memory and read during the call.
- *   page: 16, 32, 64, 128 or 256;  D: 64, 128 or 256;  blocks * page < 2^31. */
+ *   page: 16, 32, 64, 128 or 256;  D: 64, 128 or 256;  blocks * page < 2^31;
+ *   heads at most 65536. */
 typedef struct rfq_kv_cache {
     uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
     int64_t blocks, heads, page, D;
@@ -553,7 +554,7 @@ rfq_status rfq_block_release(const int32_t *lens, const uint8_t *ended, int64_t 
  * y = x with its heads rotated (rfq_rope_spec), fp32 arithmetic, rounded once to
  * dtype.  x and y are [T][H][D] of the same dtype; they may be the same tensor (with
  * the same strides) and may not overlap otherwise.
- *   D a multiple of 16, at most 512;  T, H below 2^31 (T < 2^31 / 16).
+ *   D a multiple of 16, at most 512;  T below 2^24, H at most 65536.
  */
 rfq_status rfq_rope(const rfq_heads *x, rfq_dtype dtype, int64_t T, int64_t H, int64_t D,
                     const rfq_rope_spec *rope, const rfq_heads *y, void *hip_stream);
@@ -574,6 +575,9 @@ rfq_status rfq_rope_backward(const rfq_heads *dy, rfq_dtype dtype, int64_t T, in
  *   k, v   [T][cache->heads][D] of dtype;  q, q_out [T][Hq][D] of dtype, or both
  *          NULL; rope may be NULL only without q.  q_out may be q itself.
  *   slots  [T] int32.
+ *   T * (Hq * D / 16 + heads * D / 4) below 2^32 less the rounding of a token's work
+ *   items to 256 (32 heads of q and 8 cached of 128 channels: T < 2^23);  Hq at most
+ *   65536.
  */
 rfq_status rfq_kv_append(const rfq_heads *k, const rfq_heads *v, rfq_dtype dtype, int64_t T,
                          const int32_t *slots, const rfq_kv_cache *cache,
@@ -583,7 +587,8 @@ rfq_status rfq_kv_append(const rfq_heads *k, const rfq_heads *v, rfq_dtype dtype
 /*
  * Reads slots back: k_out and v_out [n][cache->heads][D] dense, fp32 or bf16 (both
  * hold every MXFP4 value of rfq_kv_append exactly); 16-byte aligned.  A slot outside
- * the cache gives zeros, the scale byte 0xFF NaN.
+ * the cache gives zeros, the scale byte 0xFF NaN.  n times heads * D / 4 rounded up to
+ * 256 stays below 2^32.
  */
 rfq_status rfq_kv_gather(const rfq_kv_cache *cache, const int32_t *slots, int64_t n,
                          void *k_out, void *v_out, rfq_dtype out_dtype, void *hip_stream);
@@ -614,7 +619,8 @@ rfq_status rfq_kv_gather(const rfq_kv_cache *cache, const int32_t *slots, int64_
  *   workspace: device memory, 16-byte aligned, not read before it is written; with
  *            fewer than rfq_kv_attention_workspace_bytes bytes (or NULL, 0) a
  *            request's tokens are not split over workgroups.
- * Calls that share a workspace must be ordered.  T, B, Hq below 2^24, T * Hq < 2^31.
+ * Calls that share a workspace must be ordered.  T and B below 2^24, Hq at most
+ * 65536, T * Hq < 2^31.
  */
 rfq_status rfq_kv_attention(const rfq_heads *q, int64_t T, int64_t Hq, const rfq_kv_cache *cache,
                             const int32_t *block_tables, int64_t width,

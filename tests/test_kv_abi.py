@@ -161,3 +161,28 @@ def test_block_calls():
         assert call(B=2, **{k: None}) == ENULL, k
         if k != "ended":
             assert call(B=2, **{k: A + 2}) == EALIGN, k
+
+
+def test_largest_sizes():
+    """The sizes that the header names are taken (a missing pointer is what is found next),
+    the next ones refused."""
+    rope = _caller("rfq_rope", dict(x=_heads(None), dt=1, T=4, H=8, D=128, rope=_spec(),
+                                    y=_heads(None), s=None))
+    assert rope(T=(1 << 24) - 1) == ENULL and rope(T=1 << 24) == ESHAPE
+    assert rope(H=65536) == ENULL and rope(H=65537) == ESHAPE
+    append = _caller("rfq_kv_append", dict(
+        k=_heads(None), v=_heads(None), dt=1, T=4, slots=A, cache=_cache(heads=8), q=_heads(None),
+        Hq=32, rope=_spec(), q_out=_heads(None), s=None))
+    assert append(T=(1 << 23) - 1) == ENULL and append(T=1 << 23) == ESHAPE
+    assert append(Hq=65536) == ENULL and append(Hq=65537) == ESHAPE
+    assert append(cache=_cache(heads=65536)) == ENULL and append(cache=_cache(heads=65537)) == ESHAPE
+    gather = _caller("rfq_kv_gather", dict(cache=_cache(heads=8), slots=None, n=4, k=A, v=A, dt=1,
+                                           s=None))
+    assert gather(n=(1 << 24) - 1) == ENULL and gather(n=1 << 24) == ESHAPE
+    attention = _caller("rfq_kv_attention", dict(
+        q=_heads(None), T=4, Hq=8, cache=_cache(), tables=A, width=4, lens=A, starts=A, B=2,
+        max_query=1, max_seq=64, scale=0.1, causal=1, window=0, out=_heads(), lse=A, ws=A,
+        ws_bytes=1024, s=None))
+    assert attention(T=(1 << 24) - 1) == ENULL and attention(T=1 << 24) == ESHAPE
+    assert attention(B=(1 << 24) - 1) == ENULL and attention(B=1 << 24) == ESHAPE
+    assert attention(Hq=65536) == ENULL and attention(Hq=65538) == ESHAPE
