@@ -15,7 +15,7 @@ import torch
 from . import rfq as _binding
 from .rfq import (
     _FLOAT, _OUT_CODE, _U8, RFQ_BF16, RFQ_F32, Heads, KvCacheArgs, RopeSpec, _check, _dtype_code,
-    _need, _ptr, _result, _stream, load,
+    _empty, _need, _ptr, _result, _stream, load,
 )
 
 _I32 = (torch.int32,)
@@ -169,7 +169,7 @@ def rfq_block_assign(ctx_lens, new_lens, block_tables, free_blocks, free_count, 
         raise ValueError("tokens must not be negative")
 
     def new(n):
-        return torch.empty(n, dtype=torch.int32, device=ctx_lens.device)
+        return _empty(n, torch.int32, ctx_lens.device, stream)
     slots, positions, seq_lens, starts, counts = new(tokens), new(tokens), new(B), new(B + 1), new(3)
     st = load().rfq_block_assign(
         _ptr(ctx_lens), _ptr(new_lens), B, _ptr(block_tables), block_tables.shape[1],
@@ -196,7 +196,7 @@ def rfq_block_release(lens, ended, block_tables, free_blocks, free_count, page, 
     if block_tables.dim() != 2 or block_tables.shape[0] != B or free_blocks.dim() != 1:
         raise ValueError("block_tables must be [B][width] and free_blocks 1-D")
     _need(free_count, "free_count", _I32, (1,), dev)
-    count = torch.empty(1, dtype=torch.int32, device=lens.device)
+    count = _empty(1, torch.int32, lens.device, stream)
     st = load().rfq_block_release(
         _ptr(lens), _ptr(ended), B, _ptr(block_tables), block_tables.shape[1], _ptr(free_blocks),
         free_blocks.shape[0], _ptr(free_count), int(page), _ptr(count), _stream(stream, dev))
@@ -214,7 +214,7 @@ def _rope_call(func, x, positions, cos_sin, axes, interleaved, out, stream):
     T, H, D = x.shape
     spec = _rope(positions, cos_sin, axes, interleaved, T, dev)
     if out is None:
-        out = torch.empty((T, H, D), dtype=x.dtype, device=x.device)
+        out = _empty((T, H, D), x.dtype, x.device, stream)
     else:
         _need_heads(out, "out", (x.dtype,), x.shape, dev)
     st = getattr(load(), func)(ctypes.byref(_heads(x)), _dtype_code(x), T, H, D,
@@ -272,7 +272,7 @@ def rfq_kv_append(k, v, slots, cache, q=None, positions=None, cos_sin=None, axes
         if q.shape[0] != T or q.shape[2] != D:
             raise ValueError("q must be [%d][Hq][%d], not %s" % (T, D, tuple(q.shape)))
         if q_out is None:
-            q_out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
+            q_out = _empty((T, Hq, D), q.dtype, q.device, stream)
         else:
             _need_heads(q_out, "q_out", (q.dtype,), q.shape, dev)
         qa, qo = ctypes.byref(_heads(q)), ctypes.byref(_heads(q_out))
@@ -299,8 +299,7 @@ def rfq_kv_gather(cache, slots, out_dtype=torch.bfloat16, stream=None):
         raise TypeError("out_dtype must be torch.float32 or torch.bfloat16")
     dev, n = slots.get_device(), slots.shape[0]
     args = _need_cache(cache, dev)
-    k = torch.empty((n, args.heads, args.D), dtype=out_dtype, device=slots.device)
-    v = torch.empty_like(k)
+    k, v = (_empty((n, args.heads, args.D), out_dtype, slots.device, stream) for _ in range(2))
     st = load().rfq_kv_gather(ctypes.byref(args), _ptr(slots), n, _ptr(k), _ptr(v),
                               RFQ_BF16 if out_dtype == torch.bfloat16 else RFQ_F32,
                               _stream(stream, dev))
@@ -343,15 +342,15 @@ def rfq_kv_attention(q, cache, block_tables, seq_lens, query_starts, max_query, 
     _vector(seq_lens, "seq_lens", B, dev)
     _vector(query_starts, "query_starts", B + 1, dev)
     if out is None:
-        out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
+        out = _empty((T, Hq, D), q.dtype, q.device, stream)
     else:
         _need_heads(out, "out", _BF16, q.shape, dev)
-    lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device) if return_lse else None
+    lse = _empty((T, Hq), torch.float32, q.device, stream) if return_lse else None
     if workspace is None:
         nbytes = load().rfq_kv_attention_workspace_bytes(T, Hq, args.heads, D, B, int(max_query),
                                                          int(max_seq))
         if nbytes > 0:
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+            workspace = _empty(nbytes, torch.uint8, q.device, stream, returned=False)
     else:
         _need(workspace, "workspace", _U8, None, dev)
         nbytes = workspace.numel()

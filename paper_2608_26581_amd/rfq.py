@@ -242,6 +242,23 @@ def _stream(stream, dev=None):
     return torch.cuda.current_stream().cuda_stream
 
 
+def _empty(shape, dtype, device, stream, returned=True):
+    """A new tensor for work on `stream` (None: the current one).  Torch's allocator gives
+    freed memory to the next request on the same stream, and only that stream's
+    order keeps the two uses apart.  Memory for work on another stream is
+    therefore taken on that stream; what the caller gets (returned) is held for
+    its use on the current one as well."""
+    if stream is None or stream.cuda_stream == _stream(None, device.index):
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if returned:
+        t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
 def _check(func, status):
     if status != 0:
         raise RfqError(func, status)
@@ -321,16 +338,16 @@ def _shape_of_codes(codes, name):
     return codes.shape[0], codes.shape[1] * 2
 
 
-def _codes_out(rows, K, device):
-    return (torch.empty((rows, K // 2), dtype=torch.uint8, device=device),
-            torch.empty((rows, K // 32), dtype=torch.uint8, device=device))
+def _codes_out(rows, K, device, stream):
+    return (_empty((rows, K // 2), torch.uint8, device, stream),
+            _empty((rows, K // 32), torch.uint8, device, stream))
 
 
-def _outputs(out, rows, K, device, residual, name, dev=None):
+def _outputs(out, rows, K, device, residual, name, stream, dev=None):
     """Codes outputs (qc, qs, rc, rs): allocated, or the caller's checked."""
     if out is None:
-        qc, qs = _codes_out(rows, K, device)
-        rc, rs = _codes_out(rows, K, device) if residual else (None, None)
+        qc, qs = _codes_out(rows, K, device, stream)
+        rc, rs = _codes_out(rows, K, device, stream) if residual else (None, None)
         return qc, qs, rc, rs
     qc, qs, rc, rs = out
     _need_codes(qc, qs, rows, K, name + " primary", dev)
@@ -338,11 +355,11 @@ def _outputs(out, rows, K, device, residual, name, dev=None):
     return qc, qs, rc, rs
 
 
-def _z_out(out, out_dtype, M, N, device, dev=None):
+def _z_out(out, out_dtype, M, N, device, stream, dev=None):
     if out is None:
         if out_dtype not in _FLOAT:
             raise TypeError("out_dtype must be torch.float32 or torch.bfloat16")
-        return torch.empty((M, N), dtype=out_dtype, device=device)
+        return _empty((M, N), out_dtype, device, stream)
     if dev is None or not _ok(out, _FLOAT, (M, N), dev):
         _need(out, "out", _FLOAT, (M, N), dev)
     return out
@@ -360,7 +377,7 @@ def rfq_quantize_act(x, residual=True, out=None, stream=None):
     if x.dim() != 2:
         raise ValueError("x must be 2-D [M][K]")
     M, K = x.shape
-    qc, qs, rc, rs = _outputs(out, M, K, x.device, residual, "out", dev)
+    qc, qs, rc, rs = _outputs(out, M, K, x.device, residual, "out", stream, dev)
     st = load().rfq_quantize_act(_ptr(x), _dtype_code(x), M, K, _ptr(qc), _ptr(qs),
                                  _ptr(rc), _ptr(rs), _stream(stream, dev))
     _check("rfq_quantize_act", st)
@@ -374,7 +391,7 @@ def rfq_quantize_weight(w, out=None, stream=None):
         raise ValueError("w must be 2-D [N][K]")
     N, K = w.shape
     if out is None:
-        wc, ws = _codes_out(N, K, w.device)
+        wc, ws = _codes_out(N, K, w.device, stream)
     else:
         wc, ws = out
         _need_codes(wc, ws, N, K, "out")
@@ -408,11 +425,11 @@ def rfq_gemm(q_codes, q_scales, r_codes, r_scales, w_codes, w_scales,
     _need_codes(q_codes, q_scales, M, K, "q", dev)
     _need_pair(r_codes, r_scales, M, K, "r", dev)
     _need_codes(w_codes, w_scales, N, K, "w", dev)
-    z = _z_out(out, out_dtype, M, N, q_codes.device, dev)
+    z = _z_out(out, out_dtype, M, N, q_codes.device, stream, dev)
     if split:
         nbytes = load().rfq_gemm_workspace_bytes(M, N, K)
         if nbytes > 0:
-            ws = torch.empty(nbytes, dtype=torch.uint8, device=q_codes.device)
+            ws = _empty(nbytes, torch.uint8, q_codes.device, stream, returned=False)
             st = load().rfq_gemm_split(_ptr(q_codes), _ptr(q_scales), _ptr(r_codes),
                                        _ptr(r_scales), _ptr(w_codes), _ptr(w_scales), M, N, K,
                                        _ptr(z), _dtype_code(z), _ptr(ws), nbytes,
@@ -440,7 +457,7 @@ def rfq_gemm_split_noalloc(q_codes, q_scales, r_codes, r_scales, w_codes, w_scal
     _need_codes(q_codes, q_scales, M, K, "q", dev)
     _need_pair(r_codes, r_scales, M, K, "r", dev)
     _need_codes(w_codes, w_scales, N, K, "w", dev)
-    z = _z_out(out, out_dtype, M, N, q_codes.device, dev)
+    z = _z_out(out, out_dtype, M, N, q_codes.device, stream, dev)
     st = load().rfq_gemm_split_noalloc(_ptr(q_codes), _ptr(q_scales), _ptr(r_codes),
                                        _ptr(r_scales), _ptr(w_codes), _ptr(w_scales), M, N, K,
                                        _ptr(z), _dtype_code(z), _stream(stream, dev))
@@ -466,7 +483,7 @@ def rfq_gemm_split(q_codes, q_scales, r_codes, r_scales, w_codes, w_scales, work
     if workspace is not None:
         _need(workspace, "workspace", _U8, None, dev)
         nbytes = workspace.numel()
-    z = _z_out(out, out_dtype, M, N, q_codes.device, dev)
+    z = _z_out(out, out_dtype, M, N, q_codes.device, stream, dev)
     st = load().rfq_gemm_split(_ptr(q_codes), _ptr(q_scales), _ptr(r_codes), _ptr(r_scales),
                                _ptr(w_codes), _ptr(w_scales), M, N, K, _ptr(z), _dtype_code(z),
                                _ptr(workspace), nbytes, _stream(stream, dev))
@@ -492,7 +509,7 @@ def rfq_gemm_stream(x, w_codes, w_scales, residual=True, out_dtype=torch.float32
     if Kw != K:
         raise ValueError("K mismatch between activations and weight codes")
     _need_codes(w_codes, w_scales, N, K, "w", dev)
-    z = _z_out(out, out_dtype, M, N, x.device, dev)
+    z = _z_out(out, out_dtype, M, N, x.device, stream, dev)
     st = load().rfq_gemm_stream(_ptr(x), _dtype_code(x), int(bool(residual)), _ptr(w_codes),
                                 _ptr(w_scales), M, N, K, _ptr(z), _dtype_code(z),
                                 _stream(stream, dev))
@@ -518,7 +535,7 @@ def rfq_gemm_phi(q_codes, q_scales, r_codes, r_scales, w_codes, w_scales, phi,
     _need_codes(w_codes, w_scales, N, K, "w")
     if phi is not None:
         _need(phi, "phi", _U8, ((M + 63) // 64, (K + 255) // 256))
-    z = _z_out(out, out_dtype, M, N, q_codes.device)
+    z = _z_out(out, out_dtype, M, N, q_codes.device, stream)
     st = load().rfq_gemm_phi(_ptr(q_codes), _ptr(q_scales), _ptr(r_codes), _ptr(r_scales),
                              _ptr(w_codes), _ptr(w_scales), _ptr(phi), M, N, K, _ptr(z),
                              _dtype_code(z), _stream(stream))
@@ -543,7 +560,7 @@ def rfq_fallback_map(r_codes, q_scales, rule, threshold=0, out=None, stream=None
         _need(q_scales, "q scales", _U8, (M, K // 32))
     shape = ((M + 63) // 64, (K + 255) // 256)
     if out is None:
-        phi = torch.empty(shape, dtype=torch.uint8, device=q_scales.device)
+        phi = _empty(shape, torch.uint8, q_scales.device, stream)
     else:
         phi = out
         _need(phi, "out", _U8, shape)
@@ -558,7 +575,8 @@ def rfq_mfma_fp4_loop(iters, random_operands=True, sink=None, stream=None):
     CU (MFMA_LOOP_FLOPS_PER_ITER flops per iteration); returns the sink of
     one fp32 checksum per work item."""
     if sink is None:
-        sink = torch.empty(MFMA_LOOP_ITEMS, dtype=torch.float32, device="cuda")
+        sink = _empty(MFMA_LOOP_ITEMS, torch.float32,
+                      torch.device("cuda", torch.cuda.current_device()), stream)
     else:
         _need(sink, "sink", (torch.float32,), (MFMA_LOOP_ITEMS,))
     st = load().rfq_mfma_fp4_loop(int(iters), 1 if random_operands else 0, _ptr(sink),
@@ -571,7 +589,8 @@ def rfq_mfma_bf16_loop(iters, random_operands=True, sink=None, stream=None):
     """Measurement support: rfq_mfma_fp4_loop on the bf16 matrix cores
     (MFMA_BF16_LOOP_FLOPS_PER_ITER flops per iteration)."""
     if sink is None:
-        sink = torch.empty(MFMA_LOOP_ITEMS, dtype=torch.float32, device="cuda")
+        sink = _empty(MFMA_LOOP_ITEMS, torch.float32,
+                      torch.device("cuda", torch.cuda.current_device()), stream)
     else:
         _need(sink, "sink", (torch.float32,), (MFMA_LOOP_ITEMS,))
     st = load().rfq_mfma_bf16_loop(int(iters), 1 if random_operands else 0, _ptr(sink),
@@ -585,7 +604,7 @@ def rfq_dequant(codes, scales, out=None, stream=None):
     rows, K = _shape_of_codes(codes, "codes")
     _need_codes(codes, scales, rows, K, "dequantization input")
     if out is None:
-        o = torch.empty((rows, K), dtype=torch.float32, device=codes.device)
+        o = _empty((rows, K), torch.float32, codes.device, stream)
     else:
         o = out
         _need(o, "out", (torch.float32,), (rows, K))
@@ -601,8 +620,8 @@ def rfq_swiglu_quantize_act(g, u, residual=True, return_h=False, out=None, strea
     if g.shape != u.shape or g.dtype != u.dtype or g.dim() != 2:
         raise ValueError("g and u must be 2-D with the same shape and dtype")
     M, Nh = g.shape
-    qc, qs, rc, rs = _outputs(out, M, Nh, g.device, residual, "out")
-    h = torch.empty((M, Nh), dtype=torch.bfloat16, device=g.device) if return_h else None
+    qc, qs, rc, rs = _outputs(out, M, Nh, g.device, residual, "out", stream)
+    h = _empty((M, Nh), torch.bfloat16, g.device, stream) if return_h else None
     st = load().rfq_swiglu_quantize_act(_ptr(g), _ptr(u), _dtype_code(g), M, Nh, _ptr(qc),
                                         _ptr(qs), _ptr(rc), _ptr(rs), _ptr(h), _stream(stream))
     _check("rfq_swiglu_quantize_act", st)
@@ -630,9 +649,8 @@ def rfq_gemm_swiglu_quantize(q_codes, q_scales, r_codes, r_scales, wgu_codes, wg
     _need_codes(q_codes, q_scales, M, K, "q")
     _need_pair(r_codes, r_scales, M, K, "r")
     _need_codes(wgu_codes, wgu_scales, N2, K, "gate/up")
-    hqc, hqs, hrc, hrs = _outputs(out, M, Nh, q_codes.device, residual, "out")
-    h = (torch.empty((M, Nh), dtype=torch.bfloat16, device=q_codes.device)
-         if return_h else None)
+    hqc, hqs, hrc, hrs = _outputs(out, M, Nh, q_codes.device, residual, "out", stream)
+    h = _empty((M, Nh), torch.bfloat16, q_codes.device, stream) if return_h else None
     st = load().rfq_gemm_swiglu_quantize(
         _ptr(q_codes), _ptr(q_scales), _ptr(r_codes), _ptr(r_scales), _ptr(wgu_codes),
         _ptr(wgu_scales), M, Nh, K, _ptr(hqc), _ptr(hqs), _ptr(hrc), _ptr(hrs), _ptr(h),
@@ -655,9 +673,9 @@ def _need_hif4(codes, meta, rows, K, name, dev=None):
     _need(meta, name + " meta", _I32, (rows, K // 64), dev)
 
 
-def _hif4_out(rows, K, device):
-    return (torch.empty((rows, K // 2), dtype=torch.uint8, device=device),
-            torch.empty((rows, K // 64), dtype=torch.int32, device=device))
+def _hif4_out(rows, K, device, stream):
+    return (_empty((rows, K // 2), torch.uint8, device, stream),
+            _empty((rows, K // 64), torch.int32, device, stream))
 
 
 def rfq_hif4_quantize(x, residual=True, out=None, stream=None):
@@ -673,8 +691,8 @@ def rfq_hif4_quantize(x, residual=True, out=None, stream=None):
         raise ValueError("x must be 2-D [rows][K]")
     rows, K = x.shape
     if out is None:
-        qc, qm = _hif4_out(rows, K, x.device)
-        rc, rm = _hif4_out(rows, K, x.device) if residual else (None, None)
+        qc, qm = _hif4_out(rows, K, x.device, stream)
+        rc, rm = _hif4_out(rows, K, x.device, stream) if residual else (None, None)
     else:
         qc, qm, rc, rm = out
         _need_hif4(qc, qm, rows, K, "out primary", dev)
@@ -697,7 +715,7 @@ def rfq_hif4_dequant(codes, meta, out_dtype=torch.float32, out=None, stream=None
     if out is None:
         if out_dtype not in _FLOAT:
             raise TypeError("out_dtype must be torch.float32 or torch.bfloat16")
-        o = torch.empty((rows, K), dtype=out_dtype, device=codes.device)
+        o = _empty((rows, K), out_dtype, codes.device, stream)
     else:
         o = out
         _need(o, "out", _FLOAT, (rows, K), dev)
@@ -736,11 +754,11 @@ def rfq_hif4_gemm(q_codes, q_meta, r_codes, r_meta, w_codes, w_meta,
         if r is not None:
             return r
     M, N, K, dev = _hif4_operands(q_codes, q_meta, r_codes, r_meta, w_codes, w_meta)
-    z = _z_out(out, out_dtype, M, N, q_codes.device, dev)
+    z = _z_out(out, out_dtype, M, N, q_codes.device, stream, dev)
     if split:
         nbytes = load().rfq_hif4_gemm_workspace_bytes(M, N, K)
         if nbytes > 0:
-            ws = torch.empty(nbytes, dtype=torch.uint8, device=q_codes.device)
+            ws = _empty(nbytes, torch.uint8, q_codes.device, stream, returned=False)
             st = load().rfq_hif4_gemm_split(_ptr(q_codes), _ptr(q_meta), _ptr(r_codes),
                                             _ptr(r_meta), _ptr(w_codes), _ptr(w_meta), M, N, K,
                                             _ptr(z), _dtype_code(z), _ptr(ws), nbytes,
@@ -771,7 +789,7 @@ def rfq_hif4_gemm_split(q_codes, q_meta, r_codes, r_meta, w_codes, w_meta, works
     if workspace is not None:
         _need(workspace, "workspace", _U8, None, dev)
         nbytes = workspace.numel()
-    z = _z_out(out, out_dtype, M, N, q_codes.device, dev)
+    z = _z_out(out, out_dtype, M, N, q_codes.device, stream, dev)
     st = load().rfq_hif4_gemm_split(_ptr(q_codes), _ptr(q_meta), _ptr(r_codes), _ptr(r_meta),
                                     _ptr(w_codes), _ptr(w_meta), M, N, K, _ptr(z),
                                     _dtype_code(z), _ptr(workspace), nbytes,
@@ -796,7 +814,7 @@ def rfq_hif4_gemm_wbf16(q_codes, q_meta, r_codes, r_meta, w_bf16, out_dtype=torc
         raise ValueError("w_bf16 must be a 2-D tensor [N][K] with the activations' K")
     N = w_bf16.shape[0]
     _need(w_bf16, "w_bf16", (torch.bfloat16,), (N, K), dev)
-    z = _z_out(out, out_dtype, M, N, q_codes.device, dev)
+    z = _z_out(out, out_dtype, M, N, q_codes.device, stream, dev)
     st = load().rfq_hif4_gemm_wbf16(_ptr(q_codes), _ptr(q_meta), _ptr(r_codes), _ptr(r_meta),
                                     _ptr(w_bf16), M, N, K, _ptr(z), _dtype_code(z),
                                     _stream(stream, dev))
