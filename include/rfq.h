@@ -620,7 +620,7 @@ rfq_status rfq_kv_gather(const rfq_kv_cache *cache, const int32_t *slots, int64_
  *            fewer than rfq_kv_attention_workspace_bytes bytes (or NULL, 0) a
  *            request's tokens are not split over workgroups.
  * Calls that share a workspace must be ordered.  T and B below 2^24, Hq at most
- * 65536, T * Hq < 2^31.
+ * 65536, T * Hq at most 2^31 - 128.
  */
 rfq_status rfq_kv_attention(const rfq_heads *q, int64_t T, int64_t Hq, const rfq_kv_cache *cache,
                             const int32_t *block_tables, int64_t width,

@@ -83,11 +83,12 @@ rfq_status rope_call(const rfq_heads *x, rfq_dtype dtype, int64_t T, int64_t H, 
                                    static_cast<hipStream_t>(hip_stream)));
 }
 
-// A workspace query takes the sizes that the call takes.
+// A workspace query takes the sizes that the call takes.  One head and request can have all
+// T * Hq rows, in tiles of up to kWideRows: the last tile's end is a 32-bit number too.
 bool attention_sizes_ok(int64_t T, int64_t Hq, int64_t heads, int64_t B) {
-  constexpr int64_t most = int64_t(1) << 24;
+  constexpr int64_t most = int64_t(1) << 24, rows = INT32_MAX - (rfq::kWideRows - 1);
   return T >= 0 && T < most && B >= 0 && B < most && heads >= 1 && heads <= kMaxHeads &&
-         Hq >= heads && Hq <= kMaxHeads && Hq % heads == 0 && T * Hq <= INT32_MAX;
+         Hq >= heads && Hq <= kMaxHeads && Hq % heads == 0 && T * Hq <= rows;
 }
 
 }  // namespace

@@ -186,3 +186,20 @@ def test_largest_sizes():
     assert attention(T=(1 << 24) - 1) == ENULL and attention(T=1 << 24) == ESHAPE
     assert attention(B=(1 << 24) - 1) == ENULL and attention(B=1 << 24) == ESHAPE
     assert attention(Hq=65536) == ENULL and attention(Hq=65538) == ESHAPE
+
+
+def test_rows_and_tiles_stay_within_32_bits():
+    """A request may have all T * Hq rows of one cached head, in tiles of up to 128 rows
+    whose ends are counted in 32 bits: 2^31 - 1 - 127 rows at most."""
+    most = 2 ** 31 - 1 - 127
+    f = binding.load().rfq_kv_attention_workspace_bytes
+    attention = _caller("rfq_kv_attention", dict(
+        q=_heads(None), T=4, Hq=8, cache=_cache(heads=1), tables=A, width=4, lens=A, starts=A, B=2,
+        max_query=1, max_seq=64, scale=0.1, causal=1, window=0, out=_heads(), lse=A, ws=A,
+        ws_bytes=1024, s=None))
+    for Hq in (49981, 65536, 32768, 128, 129, 1000):
+        T = min(most // Hq, 2 ** 24 - 1)
+        assert attention(T=T, Hq=Hq) == ENULL, Hq
+        if T < 2 ** 24 - 1:
+            assert attention(T=T + 1, Hq=Hq) == ESHAPE and f(T + 1, Hq, 1, 64, 2, T, 4096) == 0, Hq
+    assert 42966 * 49981 < 2 ** 31 and attention(T=42966, Hq=49981) == ESHAPE
