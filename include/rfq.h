@@ -526,10 +526,12 @@ typedef struct rfq_kv_cache {
  *   counts        [3]: free blocks left, new tokens, refused requests.  counts may
  *                 not overlap free_count; its first element is the free_count of
  *                 the next call.
- * tokens may exceed the number of new tokens (a captured step of fixed size); where
- * it is smaller, the tokens past it get neither slot nor block.  page: as
- * rfq_kv_cache.  B at most 16384; B == 0 writes slots, positions, query_starts[0]
- * and counts.  Calling it again with the same inputs writes the same values.
+ * tokens may exceed the number of new tokens (a captured step of fixed size).  Where
+ * it is smaller, slots and positions end there and nothing else changes: the tokens
+ * past it have their blocks, the lengths and counts include them, and what stands in
+ * their slots has still to be written.  page: as rfq_kv_cache.  B at most 16384;
+ * B == 0 writes slots, positions, query_starts[0] and counts.  Calling it again
+ * with the same inputs writes the same values, with more tokens those of the rest.
  */
 rfq_status rfq_block_assign(const int32_t *ctx_lens, const int32_t *new_lens, int64_t B,
                             int32_t *block_tables, int64_t width, const int32_t *free_blocks,

@@ -7,7 +7,7 @@
 // request; the block is the table's where p / page < held_b, else the one taken as
 // number F_b + p / page - held_b.  Every taken block holds exactly one new token at
 // its start, so the token with p % page == 0 writes the table entry and nothing
-// is searched twice.
+// is searched twice (but for tokens that the call's `tokens` leaves out).
 //
 // The work is two int32 in and a few out per request and two out per token: a few
 // hundred KB at most, so a call costs its launch and its chain of dependent
@@ -200,6 +200,21 @@ __global__ __launch_bounds__(kThreads) void block_assign_kernel(
     }
     slots[t] = slot;
     positions[t] = pos;
+  }
+  // Tokens past `tokens` get no slot, but the blocks that begin with them are taken as all
+  // others (lengths and counts have them): a wave a request, from the one with token
+  // number `tokens` on.
+  if (all_tok > tokens) {
+    const int waves = kThreads / 64;
+    for (int b = owner(start, B, tokens) + (int)blockIdx.x * waves + (tid >> 6); b < B;
+         b += (int)gridDim.x * waves) {
+      if (first[b] < 0) continue;
+      const int64_t c = max(ctx_lens[b], 0), add = max(new_lens[b], 0);
+      const int64_t had = (c + page1) >> page_shift, need = (c + add + page1) >> page_shift;
+      for (int64_t j = had + (tid & 63); j < need; j += 64)
+        if (start[b] + (j << page_shift) - c >= tokens)
+          tables[(int64_t)b * width + j] = free_blocks[count - 1 - (first[b] + (j - had))];
+    }
   }
 }
 

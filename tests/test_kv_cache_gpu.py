@@ -358,3 +358,41 @@ def test_block_refusals():
     big = torch.zeros(16385, dtype=torch.int32, device="cuda")
     with pytest.raises(rfq.RfqError, match="SHAPE"):
         rfq.rfq_block_assign(big, big, big[:, None], f, c, 16, 2)
+
+
+@pytest.mark.parametrize("B", [1, 3, 65, 300, 1500])
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("scarce", [False, True])
+def test_assign_fewer_tokens_than_new(B, page, scarce):
+    """`tokens` cuts slots and positions and nothing else: tables, lengths and counts are
+    those of the whole step, the next step goes on from them, and release finds
+    every block that was taken, once."""
+    rng = np.random.default_rng(B + page)
+    width = 12
+    new = np.where(rng.random(B) < 0.3, 1, rng.integers(0, 100, B))
+    later = np.where(rng.random(B) < 0.7, 1, rng.integers(0, 60, B))
+    total, zero = int(new.sum()), np.zeros(B, np.int64)
+    lack = int((-(-new // page)).sum())
+    n = max(1, lack // 2) if scarce else lack + B * 5
+    free = rng.permutation(n).astype(np.int32)
+    none = np.full((B, width), -1, np.int32)
+
+    def ints(a):
+        return _dev(np.asarray(a, np.int32))
+    for tokens in sorted({0, 1, total // 2, max(0, total - 1)}):
+        t, f = ints(none), ints(free)
+        got = rfq.rfq_block_assign(ints(zero), ints(new), t, f, ints([n]), page, tokens)
+        want = _assign(zero, new, none, free, n, page, total)
+        assert np.array_equal(t.cpu().numpy(), want[5])
+        assert all(np.array_equal(g.cpu().numpy(), w) for g, w in zip(got[2:], want[2:5]))
+        assert all(np.array_equal(g.cpu().numpy(), w[:tokens]) for g, w in zip(got[:2], want[:2]))
+        seq, left = want[2], int(want[4][0])
+        got = rfq.rfq_block_assign(got[2], ints(later), t, f, got[4][:1].clone(), page,
+                                   int(later.sum()))
+        want = _assign(seq, later, want[5], free, left, page, int(later.sum()))
+        assert np.array_equal(t.cpu().numpy(), want[5])
+        assert all(np.array_equal(g.cpu().numpy(), w) for g, w in zip(got, want))
+        lens = np.where(want[2] > 0, want[2], seq)             # (a refused request keeps its own)
+        count = rfq.rfq_block_release(ints(lens), torch.ones(B, dtype=torch.uint8, device="cuda"),
+                                      t, f, got[4][:1].clone(), page)
+        assert count.item() == n and np.array_equal(np.sort(f.cpu().numpy()), np.arange(n))
