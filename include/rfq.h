@@ -521,11 +521,13 @@ typedef struct rfq_kv_cache {
  *                 for tokens of refused requests, past the last token, and in
  *                 blocks that are negative or whose slots int32 does not hold.
  *   positions     [tokens]: the token's place in its request (0 past the last).
- *   seq_lens      [B]: ctx + new, or 0 for a refused request.
+ *   seq_lens      [B]: ctx + new, or 0 for a refused request, which this step then
+ *                 leaves out.  Such a request still holds its ctx tokens: the next call's
+ *                 ctx_lens are the larger of ctx_lens and seq_lens.
  *   query_starts  [B + 1]: the requests' first rows among the new tokens.
- *   counts        [3]: free blocks left, new tokens, refused requests.  counts may
- *                 not overlap free_count; its first element is the free_count of
- *                 the next call.
+ *   counts        [3]: free blocks left, new tokens, refused requests; its first
+ *                 element is the free_count of the next call.
+ * Outputs overlap neither each other nor the inputs (block_tables is both).
  * tokens may exceed the number of new tokens (a captured step of fixed size).  Where
  * it is smaller, slots and positions end there and nothing else changes: the tokens
  * past it have their blocks, the lengths and counts include them, and what stands in

@@ -148,7 +148,9 @@ def rfq_block_assign(ctx_lens, new_lens, block_tables, free_blocks, free_count, 
     """Blocks, slots and positions of one step's tokens -> (slots [tokens],
     positions [tokens], seq_lens [B], query_starts [B + 1], counts [3]), all int32;
     block_tables [B][width] is updated.  counts: free blocks left, new tokens,
-    refused requests."""
+    refused requests.  seq_lens is 0 for a refused request, which keeps its tokens: the next
+    step's ctx_lens is torch.maximum(ctx_lens, seq_lens).  The five may be parts of one
+    allocation."""
     if stream is None:
         r = _native("block_assign", ctx_lens, new_lens, block_tables, free_blocks, free_count,
                     page, tokens)
