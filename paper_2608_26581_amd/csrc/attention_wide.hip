@@ -142,8 +142,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_wide_kerne
       }
     }
   }
-  // (At scale 0 a masked -infinity has to stay one.)
-  const float c = fabsf(a.scale_log2) < 0x1p-126f ? 0x1p-126f : fabsf(a.scale_log2);
+  // (At scale 0 a masked -infinity has to stay one, and no product, below 2^128, may show:
+  // the least fp32 value.)
+  const float c = a.scale_log2 == 0.0f ? 0x1p-149f : fabsf(a.scale_log2);
   // What all of the wave's rows see: all_lo to all_hi; the workgroup's tiles.
   auto position = [&](int row) { return req.len - req.nq + min(row, rows - 1) / a.group; };
   const int p0 = position(w0), p1 = position(w0 + S::kWaveRows - 1);

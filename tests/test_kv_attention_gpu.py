@@ -422,3 +422,15 @@ def test_refusals():
         rfq.rfq_kv_attention(torch.zeros(2 * 4 * 64 + 1, dtype=torch.bfloat16,
                                          device="cuda")[1:].view(2, 4, 64), cache, t, n, s, 2, 16)
     assert rfq.rfq_kv_attention(q[:0], cache, t, n, s, 2, 16).shape == (0, 4, 64)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_scale_zero_of_large_scores(D):
+    """At scale 0 every token weighs the same, however large its product is."""
+    rng = np.random.default_rng(19)
+    reqs = [(150, 120), (40, 1)]
+    cache = ku.Cache(rng, [n for n, _ in reqs], 2, 16, D)
+    q = _queries(rng, 121, 4, D) * 2.0 ** 120
+    out, lse = _run(q, cache, reqs, scale=0.0)
+    ref = ku.attention(q, cache, [n for n, _ in reqs], _starts(reqs), 0.0, True, 0)
+    ku.assert_attention_close(out.float().cpu().numpy(), lse.cpu().numpy(), ref)
