@@ -434,3 +434,30 @@ def test_scale_zero_of_large_scores(D):
     out, lse = _run(q, cache, reqs, scale=0.0)
     ref = ku.attention(q, cache, [n for n, _ in reqs], _starts(reqs), 0.0, True, 0)
     ku.assert_attention_close(out.float().cpu().numpy(), lse.cpu().numpy(), ref)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("n,nq,group", [(5003, 1, 1), (5003, 1, 4), (5003, 3, 8), (5003, 70, 2),
+                                        (20011, 1, 4), (20011, 40, 4), (1000, 1, 4), (1024, 9, 2)])
+def test_no_token_is_lost(D, n, nq, group):
+    """In each head one token's score stands 48 or more above the others', which are 0: each
+    row is that token's value, but for its weight's rounding and the result's to bf16
+    (2^-9 each) and the others' weights (2^15 2^-69 of at most 3 each together).  The tokens lie at
+    the ends of tiles, pages and parts."""
+    heads, page = 24, 32
+    rng = np.random.default_rng(n + nq)
+    cache = ku.Cache(rng, [n], heads, page, D)
+    at = [0, 1, 15, 16, 31, 32, 63, 64, 65, n // 3, n // 2, n - nq, n - nq - 1, n // 64 * 64 - 1,
+          n // 64 * 64 - 64, n // 256 * 256 - 1, 255, 256, 511, 512]
+    at = [min(max(j, 0), n - nq) for j in at] + [int(j) for j in rng.integers(0, n - nq + 1, heads - len(at))]
+    cache.parts[0][:] = 0
+    cache.parts[1][cache.parts[1] != 255] = 127
+    for h, j in enumerate(at):
+        cache.parts[0][cache.tables[0, j // page], h, j % page] = 0x77                  # 6 in every channel
+    q = np.ones((nq, heads * group, D))
+    out, lse = _run(q, cache, [(n, nq)])
+    want = np.stack([cache.values(0, h, n)[1][j] for h, j in enumerate(at)])
+    want = np.broadcast_to(np.repeat(want, group, 0), (nq, heads * group, D))
+    off = np.abs(out.float().cpu().numpy() - want)
+    assert np.all(off <= (2.0 ** -8 + 2.0 ** -16) * np.abs(want) + 2.0 ** -50)
+    assert np.allclose(lse.cpu().numpy(), 6 * D ** 0.5, rtol=2.0 ** -20, atol=0)
