@@ -1,5 +1,5 @@
-"""Rotary positions in training: rfq_rope and rfq_rope_backward as one autograd function,
-and a few steps that fit the projection of an image's queries to given scores.
+"""Rotary positions in training: a few steps through rfq_rope and its gradient
+(rfq_rope_backward) that fit the projection of an image's queries to given scores.
 
     python examples/rope_gradient.py [--side 16] [--steps 20]
 """
@@ -13,23 +13,6 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 import paper_2608_26581_amd as rfq  # noqa: E402
 
 
-class Rotate(torch.autograd.Function):
-    """x [T][H][D] rotated; the gradient is the rotation by the opposite angles."""
-
-    @staticmethod
-    def forward(ctx, x, positions, cos_sin, axes):
-        ctx.save_for_backward(positions, cos_sin)
-        ctx.axes = axes
-        return rfq.rfq_rope(x, positions, cos_sin, axes)
-
-    @staticmethod
-    def backward(ctx, dy):
-        positions, cos_sin = ctx.saved_tensors
-        if dy.stride(2) != 1:
-            dy = dy.contiguous()
-        return rfq.rfq_rope_backward(dy, positions, cos_sin, ctx.axes), None, None, None
-
-
 def main(side=16, steps=20, heads=4, D=64):
     torch.manual_seed(0)
     T = side * side
@@ -38,7 +21,7 @@ def main(side=16, steps=20, heads=4, D=64):
     cos_sin, axes = rfq.rope_table(side, D), rfq.rope_axes((D // 4, D // 4))
 
     def project(w):
-        return Rotate.apply((x @ w.t()).view(T, heads, D), positions, cos_sin, axes)
+        return rfq.rfq_rope((x @ w.t()).view(T, heads, D), positions, cos_sin, axes)
     x = torch.randn(T, D, device="cuda")
     keys = torch.randn(T, heads, D, device="cuda")
     target = project(torch.randn(heads * D, D, device="cuda") * D ** -0.5)

@@ -5,6 +5,8 @@ Each function carries the name of the C entry point it calls and checks its
 tensors as the other calls do.  q, k, v and outputs are [T][H][D] device tensors
 whose channels are contiguous; tokens and heads may be strided (slices of one
 joint projection).  A cache is a KvCache, or any four tensors of its layout.
+The rotation is differentiable; what goes through the 4-bit cache is not, and
+results of those calls carry no gradient.
 """
 import ctypes
 import threading
@@ -15,7 +17,7 @@ import torch
 from . import rfq as _binding
 from .rfq import (
     _FLOAT, _OUT_CODE, _U8, RFQ_BF16, RFQ_F32, Heads, KvCacheArgs, RopeSpec, _check, _dtype_code,
-    _empty, _need, _ptr, _result, _stream, load,
+    _empty, _need, _ptr, _result, _stream, _torch_stream, load,
 )
 
 _I32 = (torch.int32,)
@@ -206,7 +208,38 @@ def rfq_block_release(lens, ended, block_tables, free_blocks, free_count, page, 
     return count
 
 
+class _Rope(torch.autograd.Function):
+    """A rotation whose gradient is the rotation by the opposite angles."""
+
+    @staticmethod
+    def forward(ctx, x, positions, cos_sin, func, axes, interleaved):
+        ctx.save_for_backward(positions, cos_sin)
+        ctx.rest = func, axes, interleaved
+        return _rope_call(func, x, positions, cos_sin, axes, interleaved, None, None)
+
+    @staticmethod
+    def backward(ctx, dy):
+        func, axes, interleaved = ctx.rest
+        back = rfq_rope_backward if func == "rfq_rope" else rfq_rope
+        strides = (dy.stride(0) * dy.element_size(), dy.stride(1) * dy.element_size())
+        if dy.stride(2) != 1 or any(n % 16 for n in (dy.data_ptr(), *strides)):
+            dy = dy.clone(memory_format=torch.contiguous_format)
+        return back(dy, *ctx.saved_tensors, axes, interleaved), None, None, None, None, None
+
+
 def _rope_call(func, x, positions, cos_sin, axes, interleaved, out, stream):
+    if torch.is_grad_enabled() and isinstance(x, torch.Tensor) and (
+            x.requires_grad or getattr(out, "requires_grad", False)):
+        if out is not None:
+            raise ValueError("out takes no gradient: x and out must not require one")
+        args = (x, positions, cos_sin, func, axes, interleaved)
+        if stream is None:
+            return _Rope.apply(*args)
+        # (Autograd runs the gradient on the stream that is current here.)
+        with torch.cuda.stream(_torch_stream(stream, x.device)):
+            y = _Rope.apply(*args)
+        y.record_stream(torch.cuda.current_stream(x.device))
+        return y
     if stream is None:
         r = _native(func[4:], x, positions, cos_sin, axes, interleaved, out)
         if r is not None:
@@ -230,13 +263,14 @@ def rfq_rope(x, positions, cos_sin, axes=None, interleaved=False, out=None, stre
     """x [T][H][D] (bf16 or fp32) with its first 2 * cos_sin.shape[1] channels
     rotated: pair j of token t by cos_sin[positions[axes[j]][t]][j].  positions
     int32 [axes][T] or [T]; axes: bytes or a sequence, one entry per pair (None:
-    axis 0).  out may be x."""
+    axis 0).  out may be x.  Differentiable in x (not in cos_sin), without out."""
     return _rope_call("rfq_rope", x, positions, cos_sin, axes, interleaved, out, stream)
 
 
 def rfq_rope_backward(dy, positions, cos_sin, axes=None, interleaved=False, out=None,
                       stream=None):
-    """The gradient of rfq_rope with respect to x, from that of its result."""
+    """The gradient of rfq_rope with respect to x, from that of its result.
+    Differentiable in dy, without out."""
     return _rope_call("rfq_rope_backward", dy, positions, cos_sin, axes, interleaved, out, stream)
 
 

@@ -242,6 +242,13 @@ def _stream(stream, dev=None):
     return torch.cuda.current_stream().cuda_stream
 
 
+def _torch_stream(stream, device):
+    """stream, or a torch stream of its handle."""
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    return torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+
+
 def _empty(shape, dtype, device, stream, returned=True):
     """A new tensor for work on `stream` (None: the current one).  Torch's allocator gives
     freed memory to the next request on the same stream, and only that stream's
@@ -250,9 +257,7 @@ def _empty(shape, dtype, device, stream, returned=True):
     its use on the current one as well."""
     if stream is None or stream.cuda_stream == _stream(None, device.index):
         return torch.empty(shape, dtype=dtype, device=device)
-    if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
-    with torch.cuda.stream(stream):
+    with torch.cuda.stream(_torch_stream(stream, device)):
         t = torch.empty(shape, dtype=dtype, device=device)
     if returned:
         t.record_stream(torch.cuda.current_stream(device))

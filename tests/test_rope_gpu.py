@@ -145,3 +145,59 @@ def test_rope_table_helper():
     t = rfq.rope_table(33, 64, 500000.0)
     assert np.array_equal(t.cpu().numpy(), ku.table(33, 64, 500000.0))
     assert rfq.rope_axes((2, 0, 3)) == bytes([0, 0, 2, 2, 2])
+
+
+@pytest.mark.parametrize("f,g", [(rfq.rfq_rope, rfq.rfq_rope_backward),
+                                 (rfq.rfq_rope_backward, rfq.rfq_rope)])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_autograd(f, g, interleaved, dtype):
+    """A result of x that asks for a gradient has one: the rotation by the opposite angle, of
+    gradients with any strides, and its own gradient in turn."""
+    x, pos, axes, cs = _case(23, 4, 64, 48, 3, 8)
+    args = (_dev(pos), _dev(cs), list(axes))
+    kw = dict(interleaved=interleaved)
+    xd = _dev(x).to(dtype).requires_grad_()
+    with torch.no_grad():
+        plain = f(xd, *args, **kw)
+    assert not plain.requires_grad and not f(xd.detach(), *args, **kw).requires_grad
+    y = f(xd, *args, **kw)
+    assert y.requires_grad and torch.equal(y.detach(), plain)
+    rng = np.random.default_rng(9)
+    dy = _dev(rng.standard_normal(x.shape).astype(np.float32)).to(dtype)
+    want = g(dy, *args, **kw)
+    for grad in (dy, dy.transpose(0, 2).contiguous().transpose(0, 2),
+                 torch.cat((dy.flatten()[:1], dy.flatten()))[1:].view(dy.shape)):
+        dx, = torch.autograd.grad(y, xd, grad, retain_graph=True)
+        assert torch.equal(dx, want)
+    dx, = torch.autograd.grad(y.float().sum(), xd, retain_graph=True)      # (a broadcast 1)
+    assert torch.equal(dx, g(torch.ones_like(dy), *args, **kw))
+    v = dy.clone().requires_grad_()
+    dx, = torch.autograd.grad(y, xd, v, create_graph=True)
+    assert torch.equal(dx.detach(), want)
+    again, = torch.autograd.grad(dx, v, xd.detach())
+    assert torch.equal(again, plain)
+
+
+def test_autograd_on_a_given_stream():
+    x, pos, axes, cs = _case(50, 4, 64, 64, 2, 10)
+    args = (_dev(pos), _dev(cs), axes)
+    xd = _dev(x).requires_grad_()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    y = rfq.rfq_rope(xd, *args, stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    y.backward(y.detach())
+    torch.cuda.synchronize()
+    assert torch.equal(xd.grad, rfq.rfq_rope_backward(y.detach(), *args))
+
+
+def test_out_and_gradients():
+    """out cannot carry a gradient."""
+    x, pos, axes, cs = _case(9, 4, 64, 64, 2, 11)
+    args = (_dev(pos), _dev(cs), axes)
+    xd = _dev(x).requires_grad_()
+    with pytest.raises(ValueError, match="out"):
+        rfq.rfq_rope(xd, *args, out=torch.empty_like(x_ := xd.detach()))
+    with torch.no_grad():
+        assert torch.equal(rfq.rfq_rope(xd, *args, out=torch.empty_like(x_)), rfq.rfq_rope(x_, *args))
