@@ -17,7 +17,7 @@ import torch
 from . import rfq as _binding
 from .rfq import (
     _FLOAT, _OUT_CODE, _U8, RFQ_BF16, RFQ_F32, Heads, KvCacheArgs, RopeSpec, _check, _dtype_code,
-    _empty, _need, _ptr, _result, _stream, _torch_stream, load,
+    _empty, _need, _ptr, _result, _stream, _torch_stream, _written, load,
 )
 
 _I32 = (torch.int32,)
@@ -243,11 +243,12 @@ def _rope_call(func, x, positions, cos_sin, axes, interleaved, out, stream):
     if stream is None:
         r = _native(func[4:], x, positions, cos_sin, axes, interleaved, out)
         if r is not None:
-            return r
+            return r if out is None else _written(out)
     _need_heads(x, "x", _FLOAT)
     dev = x.get_device()
     T, H, D = x.shape
     spec = _rope(positions, cos_sin, axes, interleaved, T, dev)
+    given = out
     if out is None:
         out = _empty((T, H, D), x.dtype, x.device, stream)
     else:
@@ -256,7 +257,7 @@ def _rope_call(func, x, positions, cos_sin, axes, interleaved, out, stream):
                                ctypes.byref(spec), ctypes.byref(_heads(out)),
                                _stream(stream, dev))
     _check(func, st)
-    return out
+    return out if given is None else _written(out)
 
 
 def rfq_rope(x, positions, cos_sin, axes=None, interleaved=False, out=None, stream=None):
@@ -283,7 +284,7 @@ def rfq_kv_append(k, v, slots, cache, q=None, positions=None, cos_sin=None, axes
         r = _native("kv_append", k, v, slots, *cache, q, positions, cos_sin, axes, interleaved,
                     q_out)
         if r is not None:
-            return r[0]
+            return r[0] if q_out is None else _written(q_out)
     _need_heads(k, "k", _FLOAT)
     dev = k.get_device()
     T, heads, D = k.shape
@@ -299,7 +300,7 @@ def rfq_kv_append(k, v, slots, cache, q=None, positions=None, cos_sin=None, axes
     if positions is not None:
         spec = ctypes.byref(_rope(positions, cos_sin, axes, interleaved, T, dev))
     qa = qo = None
-    Hq = 0
+    Hq, given = 0, q_out
     if q is not None:
         if spec is None:
             raise ValueError("q is rotated: positions and cos_sin must be given")
@@ -318,7 +319,7 @@ def rfq_kv_append(k, v, slots, cache, q=None, positions=None, cos_sin=None, axes
                               _ptr(slots), ctypes.byref(args), qa, Hq, spec, qo,
                               _stream(stream, dev))
     _check("rfq_kv_append", st)
-    return q_out
+    return q_out if given is None else _written(q_out)
 
 
 def rfq_kv_gather(cache, slots, out_dtype=torch.bfloat16, stream=None):
@@ -364,6 +365,8 @@ def rfq_kv_attention(q, cache, block_tables, seq_lens, query_starts, max_query, 
                     max_seq, float(q.shape[2] ** -0.5 if scale is None else scale), causal, window,
                     return_lse, out, workspace)
         if r is not None:
+            if out is not None:
+                _written(out)
             return r if return_lse else r[0]
     _need_heads(q, "q", _BF16)
     dev = q.get_device()
@@ -377,6 +380,7 @@ def rfq_kv_attention(q, cache, block_tables, seq_lens, query_starts, max_query, 
     B, width = block_tables.shape
     _vector(seq_lens, "seq_lens", B, dev)
     _vector(query_starts, "query_starts", B + 1, dev)
+    given = out
     if out is None:
         out = _empty((T, Hq, D), q.dtype, q.device, stream)
     else:
@@ -396,4 +400,6 @@ def rfq_kv_attention(q, cache, block_tables, seq_lens, query_starts, max_query, 
         D ** -0.5 if scale is None else float(scale), bool(causal), int(window),
         ctypes.byref(_heads(out)), _ptr(lse), _ptr(workspace), nbytes, _stream(stream, dev))
     _check("rfq_kv_attention", st)
+    if given is not None:
+        _written(out)
     return (out, lse) if return_lse else out

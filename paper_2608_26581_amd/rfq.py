@@ -264,6 +264,14 @@ def _empty(shape, dtype, device, stream, returned=True):
     return t
 
 
+def _written(out):
+    """out, given by the caller and written: autograd is told, which may hold it for a
+    backward pass."""
+    if not out.is_inference():
+        torch.autograd.graph.increment_version(out)
+    return out
+
+
 def _check(func, status):
     if status != 0:
         raise RfqError(func, status)

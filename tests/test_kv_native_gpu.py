@@ -111,3 +111,21 @@ def test_other_forms_go_through_python():
         rfq.rfq_kv_gather(cache[:3], slots)
     with pytest.raises(ValueError, match="channels"):
         rfq.rfq_kv_attention(q[..., :0], cache, slots[None], slots[:1], slots[:2], 1, 1, scale=1.0)
+
+
+def test_given_outputs_count_as_written():
+    """A tensor saved for a backward pass and then given as an output is noticed there."""
+    T, q, k, v, cache = _inputs()
+    slots = torch.arange(T, dtype=torch.int32, device="cuda")
+    pos, cs = slots % 9, rfq.rope_table(9, 128)
+    tables = torch.arange(2, dtype=torch.int32, device="cuda")[None]
+    lens, starts = torch.tensor([T], dtype=torch.int32, device="cuda"), slots[[0, -1]] + slots[:2]
+    for stream in (None, torch.cuda.current_stream()):
+        out = torch.empty_like(q)
+        seen = out._version
+        rfq.rfq_kv_append(k, v, slots, cache, q=q, positions=pos, cos_sin=cs, q_out=out,
+                          stream=stream)
+        assert out._version > seen
+        seen = out._version
+        rfq.rfq_kv_attention(q, cache, tables, lens, starts, T, T, out=out, stream=stream)
+        assert out._version > seen

@@ -201,3 +201,20 @@ def test_out_and_gradients():
         rfq.rfq_rope(xd, *args, out=torch.empty_like(x_ := xd.detach()))
     with torch.no_grad():
         assert torch.equal(rfq.rfq_rope(xd, *args, out=torch.empty_like(x_)), rfq.rfq_rope(x_, *args))
+
+
+def test_what_is_written_in_place_is_noticed():
+    """A tensor saved for a backward pass and then given as out makes that pass fail."""
+    x, pos, axes, cs = _case(9, 4, 64, 64, 2, 11)
+    args, x_ = (_dev(pos), _dev(cs), axes), _dev(x)
+    for f in (rfq.rfq_rope, rfq.rfq_rope_backward):
+        for stream in (None, torch.cuda.current_stream()):
+            w = torch.ones_like(x_, requires_grad=True)
+            h = x_.clone()
+            z = (w * h).sum()
+            assert f(h, *args, out=h, stream=stream) is h
+            with pytest.raises(RuntimeError, match="inplace"):
+                z.backward()
+    with torch.inference_mode():
+        h = x_.clone()
+        assert torch.equal(rfq.rfq_rope(h, *args, out=h), rfq.rfq_rope(x_, *args))
