@@ -573,9 +573,10 @@ rfq_status rfq_rope_backward(const rfq_heads *dy, rfq_dtype dtype, int64_t T, in
  * to MXFP4 and stored in slots[t].  The codes are those of rfq_quantize_act on the
  * rotated fp32 values, which are not rounded in between.  A block that holds an
  * infinity or a NaN gets the scale byte 0xFF (NaN) and zero codes.  Tokens whose
- * slot is outside the cache (negative: padding) are not stored; of two tokens with
- * the same slot either may be the one kept.  With q given, q_out receives q rotated,
- * as rfq_rope, for every token.
+ * slot is outside the cache (negative: padding) are not stored.  A slot is named
+ * once: of several tokens with the same one, codes and scales may remain from
+ * different tokens.  With q given, q_out receives q rotated, as rfq_rope, for
+ * every token.
  *   k, v   [T][cache->heads][D] of dtype;  q, q_out [T][Hq][D] of dtype, or both
  *          NULL; rope may be NULL only without q.  q_out may be q itself.
  *   slots  [T] int32.

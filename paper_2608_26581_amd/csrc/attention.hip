@@ -11,11 +11,15 @@
 // folded into the scale.
 //
 // Codes are decoded to bf16 in registers (exact: two significant bits and a
-// power-of-two scale) and multiplied by the bf16 matrix cores with fp32 sums; P is
-// rounded to bf16 for its product (2^-9 of each weight), l adds the unrounded fp32
-// weights.  The FP4 matrix instructions could take the keys' codes as they are against
-// q split in two FP8 terms, but their sums keep about 2^-18 of the terms' sum (measured
-// on 16 x 16 x 128; bf16: 2^-25), which shows in lse.
+// power-of-two scale) and multiplied by the bf16 matrix cores with fp32 sums; l adds the
+// fp32 weights, and for its product P is rounded to bf16 (2^-9 of each weight).  What that
+// rounding drops as a second bf16 operand costs 4 to 7% here, and registers that spill (64
+// ragged requests 24.7 -> 25.8 us a pass, 4 of 131072 tokens 122.5 -> 131.2), and takes the
+// error against 64 bits from 0.0016 to 0.0015, which is the bf16 result's own.
+//
+// The FP4 matrix instructions could take the keys' codes as they are against q split in
+// two FP8 terms, but their sums keep about 2^-18 of the terms' sum (measured on
+// 16 x 16 x 128; bf16: 2^-25), which shows in lse.
 //
 // What the rows share, the codes, is the traffic: D + D / 16 bytes a token and head for
 // keys and values.  A wave reads them in the order of memory, 1 KB a load; the keys go
@@ -24,11 +28,11 @@
 // heads are one line of work cut into equal shares, one a workgroup, whatever the lengths
 // are; items that a cut divides are joined by a second kernel.
 //
-// Measured, 8 cached heads of 128 channels, 32 of q: 4 requests of 131072 tokens in 119.5 us
-// and the join 6.5 (4.8 TB/s of the 5.1 that a large copy reaches on the card: bandwidth
-// bounds it); 64 requests of 1 to 8192 tokens, 54670 in all, 21.3 + 4.5 us (latency: a
-// share is a few steps of a wave); one of 700 tokens, whole items, 10.1 us (latency: the
-// lookups, three loads of codes one after another, and joining the waves).
+// Measured, 8 cached heads of 128 channels: 4 requests of 131072 tokens, 40 heads of q, in
+// 119.7 us and the join 6.6 (4.8 TB/s of the 5.1 that a large copy reaches on the card:
+// bandwidth bounds it); with 32 of q 64 requests of 1 to 8192 tokens, 54670 in all, 20.4 + 4.8
+// us (latency: a share is a few steps of a wave); one of 700 tokens, whole items, 9.8 us
+// (latency: the lookups, three loads of codes one after another, and joining the waves).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -647,7 +651,7 @@ hipError_t launch(const AttentionArgs &a, unsigned groups, float *work, hipStrea
 // the wide kernel, unless every request must have more (their sum and the largest say so;
 // then a wrong hint costs time only, since the wide kernel takes rows of any number): two
 // pieces of prompts over 16000 tokens take 9 us less without the other kernel's launches.
-// Eight requests of 64 rows over 3000 tokens take 33.8 us here and 40.4 in the wide
+// Of 128 channels, eight requests of 64 rows over 3000 tokens take 33.8 us here and 40.4 in the wide
 // kernel, of 128 rows 48.6 and 49.1, of 256 rows and 60000 tokens 912 and 885.
 constexpr int kFewRows = 64;
 struct Plan {
@@ -661,11 +665,15 @@ struct Plan {
 };
 
 // Few items of few tokens are not split: a workgroup of eight waves an item.  Measured, 8
-// heads of 128 channels, unsplit and split: one request of 500 tokens 8.9 and 10.8 us, of
-// 1000 11.6 and 10.9, of 2000 17.3 and 12.8; 16 of 900 11 and 15; 64 of 500 19.2 and 22.4;
-// 400 of 500 117 and 62.  Tiles have 16 rows there, else 32 if a request's rows fill them
-// and the registers allow: 24 rows over 500 tokens 9.3 us and with 32 16.8, but for 64
-// requests 35.9 and 21.7, which stay whole up to 256 tokens (of 100: 12.5 us, split 19.6).
+// cached heads and one query of 32, whole and split with the join (us):
+//   requests x tokens  1 x 500     1 x 1000    1 x 2000    16 x 900    64 x 500   400 x 500
+//   64 channels         7.4  10.5   9.6  10.5  13.9  10.5   9.8  12.8  10.4 15.1   61  43
+//   128                 8.3  11.7  11.1  11.8  16.7  11.8  11.3  14.7  19.1 19.4  117  60
+//   256                12.9  15.6  19.3  15.9  31.5  15.9  19.9  22.9  29.3 25.9  195 142
+// The lines are drawn for 128 channels; for 256 they would be lower, by up to 3.4 us a call.
+// Tiles have 16 rows there, else 32 if a request's rows fill them and the registers allow
+// (128 channels): 24 rows over 500 tokens 9.3 us and with 32 16.8, but for 64 requests 35.9 and
+// 21.7, which stay whole up to 256 tokens (of 100: 12.5 us, split 19.6).
 constexpr int64_t kFewItems = 512, kFewTokens = 1024;
 void plan_few(Plan &p, int64_t T, int64_t group, int64_t heads, int64_t D, int64_t B, int64_t rows,
               int64_t max_seq) {

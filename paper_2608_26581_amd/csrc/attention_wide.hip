@@ -9,11 +9,14 @@
 // its own.  32 x 32 x 16 products: a lane holds one row's scores of half a tile's
 // tokens, the other half is in lane ^ 32, and P again goes from one product to the next
 // in the lane's registers, rounded to the products' bf16 (2^-9 of each weight; the sum l
-// adds the unrounded weights in fp32).
+// adds the unrounded weights in fp32).  With what that rounding drops as a second operand
+// the error against 64 bits is the bf16 result's own (0.0016, else 0.0023), but the products
+// are half as many again: a prompt of 8192 tokens 807 us for 536 on the same card, two pieces
+// of prompts 153 for 107.
 //
-// Measured, 32 heads over 8 cached heads of 128 channels: a prompt of 8192 tokens in 545
-// us, 1010 TFLOP/s of the 1225 that a large bf16 product reaches on the card.  The issue
-// of instructions bounds it: the matrix units are busy 48% and the vector units 60% of
+// Measured, 32 heads over 8 cached heads of 128 channels: a prompt of 8192 tokens in 556
+// us, 988 TFLOP/s of the 1225 that a large bf16 product reaches on the card.  The issue
+// of instructions bounds it: the matrix units are busy 46% and the vector units 60% of
 // the time, the exponentials and the maximum standing against each 32 products.  Eight waves of 32
 // rows, 64 rows a wave and operands read 2 or 4 products ahead are not faster.
 #include <hip/hip_runtime.h>

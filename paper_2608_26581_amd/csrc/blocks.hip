@@ -14,8 +14,8 @@
 // loads.  Every workgroup therefore repeats the prefix sums of all requests
 // (a few values a thread, 16 bytes a request from L2) instead of a second launch
 // that would wait for a first; no workgroup reads what another writes.  Measured: one new
-// token of each of 16 requests 3.7 us, 2000 requests with 126000 new tokens 8.0 us; the blocks
-// of 500 requests given back in 4.3 us.
+// token of each of 16 requests 3.5 us, 2000 requests with 128540 new tokens 7.7 us; the blocks
+// of 500 requests given back in 4.4 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -29,8 +29,8 @@ namespace rfq {
 namespace {
 
 // Workgroups of 256 work items, or with many requests of 1024: a request's lengths are a
-// round trip to L2 apart where a thread has several (2000 requests, 126000 tokens: 12.7 us
-// with 256, 8.0 with 1024 and loads in fours).
+// round trip to L2 apart where a thread has several (2000 requests, 128540 tokens: 12.7 us
+// with 256, 7.7 with 1024 and loads in fours).
 constexpr int kFewThreads = 256, kManyThreads = 1024;
 constexpr int kTokensPerGroup = 1024;
 constexpr int kBatch = 4;                   // requests whose lengths are loaded together

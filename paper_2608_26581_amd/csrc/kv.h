@@ -13,7 +13,7 @@ rfq_status check_device();
 
 // Requests of one call to the block calls: two int32 per request in LDS.
 constexpr int64_t kMaxBlockRequests = 16384;
-// Heads of the cache's operators.
+// Channels of a head, at most, and position axes.
 constexpr int kMaxHeadDim = 512;
 constexpr int kMaxAxes = 8;
 

@@ -147,8 +147,8 @@ __device__ __forceinline__ Unit unit_of(int u, int half, bool interleaved) {
 // y = rotated x.  A workgroup takes `tokens` tokens; thread = (token, head lane,
 // unit), stepping over the heads four at a time so that four heads' loads are in
 // flight.  Bandwidth bounds it: 32768 tokens of 40 heads of 128 channels (bf16, three
-// axes, the gradient's direction) in 129.6 us, 5.2 TB/s read and written, which is what
-// a large copy reaches on the card; 1000 tokens of 40 heads take 6.0 us, launch included.
+// axes, the gradient's direction) in 131 us, 5.1 TB/s read and written, which is what
+// a large copy reaches on the card; 1000 tokens of 40 heads take 5.6 us.
 constexpr int kRopeBatch = 4;
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void rope_kernel(const uint8_t *x, int64_t x_ts,
@@ -254,7 +254,7 @@ struct Heads {
 
 // One token of a step.  Bandwidth bounds a large step: 8192 tokens, 32 heads of q and 8 of
 // k and v of 128 channels (bf16), 177 MB in 33 us, 5.4 TB/s where a large copy reaches 5.1.
-// 16 tokens take 3.5 us: the launch and the position's, the angle's and the value's way.
+// 16 tokens take 3.4 us: the launch and the position's, the angle's and the value's way.
 //
 // Work items of a token: the units of q (16 channels), then
 // the 8-channel pieces of k, then those of v, each class rounded up to whole waves;
@@ -352,7 +352,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(
 }
 
 // 8 channels of one (slot, k or v, head) a thread.  Bandwidth bounds it, four bytes written
-// for one read: 8192 slots of 8 heads of 128 channels to bf16, 42 MB, in 10.7 us; 16 in 2.8.
+// for one read: 8192 slots of 8 heads of 128 channels to bf16, 42 MB, in 10.8 us; 16 in 2.6.
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void kv_gather_kernel(const Cache cache,
                                                              const int32_t *__restrict__ slots,
