@@ -213,9 +213,10 @@ class _Rope(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, x, positions, cos_sin, func, axes, interleaved):
+        y = _rope_call(func, x, positions, cos_sin, axes, interleaved, None, None)
         ctx.save_for_backward(positions, cos_sin)
         ctx.rest = func, axes, interleaved
-        return _rope_call(func, x, positions, cos_sin, axes, interleaved, None, None)
+        return y
 
     @staticmethod
     def backward(ctx, dy):

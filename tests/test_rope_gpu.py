@@ -218,3 +218,15 @@ def test_what_is_written_in_place_is_noticed():
     with torch.inference_mode():
         h = x_.clone()
         assert torch.equal(rfq.rfq_rope(h, *args, out=h), rfq.rfq_rope(x_, *args))
+
+
+def test_refused_arguments_of_a_differentiable_call():
+    """The same errors as without a gradient."""
+    x, pos, axes, cs = _case(4, 2, 64, 64, 1, 12)
+    xd, p, c = _dev(x).requires_grad_(), _dev(pos), _dev(cs)
+    for bad, error in (((None, c), ValueError), ((p.long(), c), TypeError), ((p, None), ValueError),
+                       ((p[:, :3], c), ValueError), ((p, c, bytes(31)), ValueError),
+                       ((p, c, bytes([1] * 32)), rfq.RfqError)):
+        for a in (xd, xd.detach()):
+            with pytest.raises(error):
+                rfq.rfq_rope(a, *bad)
