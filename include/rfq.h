@@ -640,6 +640,121 @@ int64_t rfq_kv_attention_workspace_bytes(int64_t T, int64_t Hq, int64_t heads, i
                                          int64_t B, int64_t max_query, int64_t max_seq);
 
 /*
+ * A layer whose MLP is a set of experts.  A router gives every token k of E experts and
+ * their weights (rfq_route); the (token, choice) pairs are sorted by expert
+ * (rfq_expert_sort); a product takes each pair's activation row against its expert's
+ * weights (rfq_gemm_experts, for the gate and up products straight from the tokens' codes
+ * through `rows`); rfq_swiglu_quantize_act and a second product follow on the sorted rows;
+ * and the results return to the tokens, weighted (rfq_expert_combine).  Nothing is read
+ * back to the host, so the chain can be captured.
+ *
+ * T tokens with k choices are P = T * k pairs, pair t * k + j being token t's choice j;
+ * T * k below 2^31, k at most 16, E at most 1024.  Slots 0 .. P - 1 are the places of pairs
+ * in sorted order; a dropped pair has none.
+ *   offsets [E + 1]  the slots of expert e are offsets[e] .. offsets[e + 1] - 1.
+ *   rows    [P]      the token of each slot, -1 past the last.
+ *   slots   [T][k]   the slot of each pair, -1 for a dropped one.
+ */
+
+/*
+ * The k largest of each token's logits, in descending order, and their softmax weights.
+ * Of equal logits the lower index comes first; -infinity marks an expert that is not to be
+ * chosen: where a token has fewer than k others, the rest of its choices are expert -1 with
+ * weight 0.  With renormalize nonzero the weights are the softmax over the chosen logits,
+ * otherwise over all of them.  A NaN counts as larger than every number, and a token with one
+ * gets NaN weights, as does one with +infinity.  fp32 arithmetic.
+ *   logits   [T][E] dtype;  E at least k.
+ *   weights  [T][k] fp32;  experts [T][k].
+ * Pointers are aligned to their elements.  T at most 2^26 - 5.
+ */
+rfq_status rfq_route(const void *logits, rfq_dtype dtype, int64_t T, int64_t E, int64_t k,
+                     int renormalize, float *weights, int32_t *experts, void *hip_stream);
+
+/*
+ * The gradient of rfq_route's weights with respect to the logits: dlogits [T][E] of dtype
+ * from dweights [T][k], weights and experts being what rfq_route returned for these logits
+ * (with renormalize nonzero the logits are not read).  An expert that is not in [0, E) adds
+ * nothing.  fp32 arithmetic, rounded once.
+ */
+rfq_status rfq_route_backward(const float *dweights, const void *logits, rfq_dtype dtype,
+                              int64_t T, int64_t E, int64_t k, const float *weights,
+                              const int32_t *experts, int renormalize, void *dlogits,
+                              void *hip_stream);
+
+/*
+ * Sorts the pairs by expert, those of an expert in their order.  Expert first + e is number
+ * e; pairs whose expert is not in [first, first + E) are dropped (a padded token, or another
+ * device's expert).  Writes offsets, rows and slots as above; T == 0 writes offsets.
+ *   experts    [T][k].  A token may name an expert more than once.
+ *   workspace: device memory, 16-byte aligned, not read before it is written; with fewer than
+ *              rfq_expert_sort_workspace_bytes bytes (or NULL, 0) one workgroup sorts.
+ * E at least 1; first fits 32 bits.  Calls that share a workspace must be ordered.
+ */
+rfq_status rfq_expert_sort(const int32_t *experts, int64_t T, int64_t k, int64_t first, int64_t E,
+                           int32_t *offsets, int32_t *rows, int32_t *slots, void *workspace,
+                           int64_t workspace_bytes, void *hip_stream);
+
+/* Workspace of rfq_expert_sort for these sizes (0: one workgroup sorts).  Host-only. */
+int64_t rfq_expert_sort_workspace_bytes(int64_t T, int64_t k, int64_t E);
+
+/*
+ * out[s] = x[rows[s]], a copy of the row; zeros where rows[s] is not in [0, T).
+ *   x [T][N], out [P][N] of dtype, 16-byte aligned;  rows [P].
+ * Rows take ceil(N / 512) of bf16 or ceil(N / 256) of fp32 (where N is not a multiple of 8,
+ * or 4: ceil(N / 64)) units of work, which together stay below 2^26 - 4; the same holds for
+ * the rows that rfq_expert_combine and its gradient go through (T).
+ */
+rfq_status rfq_expert_gather(const void *x, rfq_dtype dtype, int64_t T, int64_t N,
+                             const int32_t *rows, int64_t P, void *out, void *hip_stream);
+
+/*
+ * out[t] = sum_j weights[t][j] z[slots[t][j]] over the pairs whose slot is in [0, P); fp32
+ * sums in the order of j, rounded once.  With ones as weights the gradient of
+ * rfq_expert_gather.
+ *   z [P][N], out [T][N] of dtype, 16-byte aligned;  slots [T][k];  weights [T][k] fp32 or
+ *   NULL (ones).
+ */
+rfq_status rfq_expert_combine(const void *z, rfq_dtype dtype, int64_t P, int64_t N,
+                              const int32_t *slots, const float *weights, int64_t T, int64_t k,
+                              void *out, void *hip_stream);
+
+/*
+ * The gradients of rfq_expert_combine: dz[slots[t][j]] = weights[t][j] dout[t], zeros in the
+ * rows of dz whose rows[s] is not in [0, T); dweights[t][j] = dout[t] . z[slots[t][j]] (fp32
+ * sums in a fixed order), 0 for a pair whose slot is not in [0, P).  rows and slots belong
+ * together, as rfq_expert_sort writes them: a slot is named once.
+ *   dout [T][N], z and dz [P][N] of dtype, 16-byte aligned;  rows [P] (read for dz only).
+ *   dz or dweights may be NULL;  z is read for dweights only.
+ *   T + P / 64 at most 2^24 - 2.
+ */
+rfq_status rfq_expert_combine_backward(const void *dout, const void *z, rfq_dtype dtype, int64_t P,
+                                       int64_t N, const int32_t *rows, const int32_t *slots,
+                                       const float *weights, int64_t T, int64_t k, void *dz,
+                                       float *dweights, void *hip_stream);
+
+/*
+ * The RFQ product of rfq_gemm with a weight matrix per expert:
+ *   Z[s][n] = sum_k (deq q + deq r)[m][k] deq(w)[e][n][k],  offsets[e] <= s < offsets[e + 1],
+ * with m = rows[s], or m = s where rows is NULL.  A row index that is not in [0, M) counts as
+ * a row of zeros.  Rows of z that belong to no expert are not written.  Accumulation is fp32
+ * in an unspecified order that does not change from call to call; codes whose products
+ * overflow or whose scale byte is 0xFF reach only their own row or column of the result.
+ *   q_codes [M][K/2], q_scales [M][K/32];  r_codes, r_scales the residual's, or both NULL.
+ *   w_codes [E][N][K/2], w_scales [E][N][K/32]: rfq_quantize_weight of [E * N][K].
+ *   offsets [E + 1], not decreasing and cut to [0, P];  rows [P] or NULL (then P == M).
+ *   z       [P][N] row-major, z_dtype.
+ * Codes, scales and z are 16-byte aligned.  The codes of the activations and those of one
+ * expert stay below 2 GiB each; M, P + 256 and N + 256 below 2^31; min(P, P / 16 + E) *
+ * ceil(N / 16) below 2^31 - 2^20.
+ */
+rfq_status rfq_gemm_experts(const uint8_t *q_codes, const uint8_t *q_scales,
+                            const uint8_t *r_codes, const uint8_t *r_scales,
+                            const uint8_t *w_codes, const uint8_t *w_scales,
+                            const int32_t *offsets, const int32_t *rows, int64_t M, int64_t P,
+                            int64_t E, int64_t N, int64_t K, void *z, rfq_dtype z_dtype,
+                            void *hip_stream);
+
+/*
  * Measurement support, not a step of the method: the sustained rate of the
  * FP4 matrix cores that the product (Eq. 11) runs on, without memory
  * traffic.  256 workgroups of 8 waves (one per CU of the MI355X, two waves

@@ -17,3 +17,8 @@ from .kv import (  # noqa: F401
     rfq_kv_attention_workspace_bytes, rfq_kv_gather, rfq_rope, rfq_rope_backward, rope_axes,
     rope_table,
 )
+from .experts import (  # noqa: F401
+    ExpertPlan, rfq_expert_combine, rfq_expert_combine_backward, rfq_expert_gather,
+    rfq_expert_sort, rfq_expert_sort_workspace_bytes, rfq_gemm_experts, rfq_route,
+    rfq_route_backward,
+)

@@ -1,0 +1,274 @@
+// The way of a layer's rows to the experts and back, and its gradients:
+//     gather    xs[s] = x[rows[s]]                    (0 where rows[s] is no row)
+//     combine   out[t] = sum_j w[t][j] z[slots[t][j]] (slots that are none: nothing)
+//     backward  dz[slots[t][j]] = w[t][j] dout[t],  dw[t][j] = dout[t] . z[slots[t][j]],
+//               dz[s] = 0 where rows[s] is no row.
+// The gradient of gather is combine with weights of one.
+//
+// All are bound by memory: every element is read and written once, 16 bytes a lane where
+// rows are whole multiples of 16 bytes.  Sums are fp32, in the order of j and, for dw, in a
+// fixed tree over the row; no atomics.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "experts.h"
+#include "gemm_common.h"
+
+namespace rfq {
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+
+// V consecutive elements (16 bytes, or one element) as fp32.
+template <bool BF16, bool VEC>
+struct Piece {
+  static constexpr int kElem = BF16 ? 2 : 4;
+  static constexpr int V = VEC ? 16 / kElem : 1;
+  using Raw = std::conditional_t<VEC, u32x4, std::conditional_t<BF16, uint16_t, uint32_t>>;
+  static __device__ __forceinline__ Raw load(const void *p, int64_t i) {
+    return static_cast<const Raw *>(p)[i];
+  }
+  static __device__ __forceinline__ void store(void *p, int64_t i, Raw v) {
+    static_cast<Raw *>(p)[i] = v;
+  }
+  static __device__ __forceinline__ void widen(Raw r, float (&f)[V]) {
+    if constexpr (!VEC) {
+      f[0] = __uint_as_float(BF16 ? (uint32_t)r << 16 : (uint32_t)r);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (BF16) {
+          f[2 * i] = __uint_as_float(r[i] << 16);
+          f[2 * i + 1] = __uint_as_float(r[i] & 0xFFFF0000u);
+        } else {
+          f[i] = __uint_as_float(r[i]);
+        }
+      }
+    }
+  }
+  static __device__ __forceinline__ Raw narrow(const float (&f)[V]) {
+    if constexpr (!VEC) {
+      if constexpr (BF16) return (Raw)bf16_rne(f[0]);
+      else return (Raw)__float_as_uint(f[0]);
+    } else {
+      u32x4 r;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (BF16) r[i] = bf16x2_rne(f[2 * i], f[2 * i + 1]);
+        else r[i] = __float_as_uint(f[i]);
+      }
+      return r;
+    }
+  }
+};
+
+// A wave's part of a row: kPieces pieces a lane, `parts` of them a row.
+constexpr int kPieces = 4;
+
+// Row and part of work item w (a wave's): rows first.
+struct Item { int64_t row; int part; };
+__device__ __forceinline__ bool item_of(int64_t rows, int parts, Item &it) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t w = (int64_t)blockIdx.x * kWaves + wave;
+  it.row = w / parts;
+  it.part = (int)(w - it.row * parts);
+  return it.row < rows;
+}
+
+template <bool BF16, bool VEC>
+__global__ __launch_bounds__(kThreads) void expert_gather_kernel(
+    const void *__restrict__ x, int64_t T, int pieces, const int32_t *__restrict__ rows, int64_t P,
+    int parts, void *__restrict__ out) {
+  using Q = Piece<BF16, VEC>;
+  Item it;
+  if (!item_of(P, parts, it)) return;
+  const int lane = threadIdx.x & 63;
+  const int64_t t = rows[it.row];
+  const bool has = t >= 0 && t < T;
+  typename Q::Raw v[kPieces] = {};
+  int c[kPieces];
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) {
+    c[i] = (it.part * kPieces + i) * 64 + lane;
+    if (has && c[i] < pieces) v[i] = Q::load(x, t * pieces + c[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i)
+    if (c[i] < pieces) Q::store(out, it.row * pieces + c[i], v[i]);
+}
+
+// One piece a lane; the rows of kBatch choices are loaded together.
+template <bool BF16, bool VEC>
+__global__ __launch_bounds__(kThreads) void expert_combine_kernel(
+    const void *__restrict__ z, int64_t P, int pieces, const int32_t *__restrict__ slots,
+    const float *__restrict__ weights, int64_t T, int k, int parts, void *__restrict__ out) {
+  using Q = Piece<BF16, VEC>;
+  constexpr int kBatch = 4;
+  Item it;
+  if (!item_of(T, parts, it)) return;
+  const int c = it.part * 64 + (threadIdx.x & 63);
+  if (c >= pieces) return;
+  float acc[Q::V] = {};
+  for (int j0 = 0; j0 < k; j0 += kBatch) {
+    typename Q::Raw v[kBatch];
+    bool has[kBatch];
+    float w[kBatch];
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      const int64_t at = it.row * k + min(j0 + b, k - 1);
+      const int64_t s = slots[at];
+      has[b] = j0 + b < k && s >= 0 && s < P;
+      w[b] = weights ? weights[at] : 1.0f;
+      if (has[b]) v[b] = Q::load(z, s * pieces + c);
+    }
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      if (has[b]) {
+        float f[Q::V];
+        Q::widen(v[b], f);
+#pragma unroll
+        for (int i = 0; i < Q::V; ++i) acc[i] = fmaf(w[b], f[i], acc[i]);
+      }
+    }
+  }
+  Q::store(out, it.row * pieces + c, Q::narrow(acc));
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+
+// A workgroup a token; those past the tokens write the zeros of dz, 64 slots each.
+template <bool BF16, bool VEC, int kMost>
+__global__ __launch_bounds__(kThreads) void expert_combine_backward_kernel(
+    const void *__restrict__ dout, const void *__restrict__ z, int64_t P, int pieces,
+    const int32_t *__restrict__ rows, const int32_t *__restrict__ slots,
+    const float *__restrict__ weights, int64_t T, int k, void *__restrict__ dz,
+    float *__restrict__ dweights) {
+  using Q = Piece<BF16, VEC>;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if ((int64_t)blockIdx.x >= T) {
+    const int64_t s0 = ((int64_t)blockIdx.x - T) * 64;
+    for (int i = 0; i < 64 && s0 + i < P; ++i) {
+      const int64_t r = rows[s0 + i];
+      if (r >= 0 && r < T) continue;
+      for (int c = tid; c < pieces; c += kThreads)
+        Q::store(dz, (s0 + i) * pieces + c, typename Q::Raw{});
+    }
+    return;
+  }
+  const int64_t t = blockIdx.x;
+  int64_t slot[kMost];
+  float w[kMost], dot[kMost];
+#pragma unroll
+  for (int j = 0; j < kMost; ++j) {
+    const int64_t s = j < k ? slots[t * k + j] : -1;
+    slot[j] = s < P ? s : -1;
+    w[j] = j < k && weights ? weights[t * k + j] : 1.0f;
+    dot[j] = 0.0f;
+  }
+  for (int c = tid; c < pieces; c += kThreads) {
+    float d[Q::V];
+    Q::widen(Q::load(dout, t * pieces + c), d);
+    typename Q::Raw v[kMost];
+    if (dweights) {
+#pragma unroll
+      for (int j = 0; j < kMost; ++j)
+        if (slot[j] >= 0) v[j] = Q::load(z, slot[j] * pieces + c);
+    }
+#pragma unroll
+    for (int j = 0; j < kMost; ++j) {
+      if (slot[j] < 0) continue;
+      if (dweights) {
+        float f[Q::V];
+        Q::widen(v[j], f);
+#pragma unroll
+        for (int i = 0; i < Q::V; ++i) dot[j] = fmaf(d[i], f[i], dot[j]);
+      }
+      if (dz) {
+        float g[Q::V];
+#pragma unroll
+        for (int i = 0; i < Q::V; ++i) g[i] = w[j] * d[i];
+        Q::store(dz, slot[j] * pieces + c, Q::narrow(g));
+      }
+    }
+  }
+  if (!dweights) return;
+  __shared__ float part[kWaves][kMost];
+#pragma unroll
+  for (int j = 0; j < kMost; ++j) {
+    const float s = wave_sum(dot[j]);
+    if (lane == 0) part[wave][j] = s;
+  }
+  __syncthreads();
+  if (tid < k) {
+    float s = part[0][tid];
+#pragma unroll
+    for (int v = 1; v < kWaves; ++v) s += part[v][tid];
+    dweights[t * k + tid] = s;
+  }
+}
+
+bool whole_pieces(int64_t N, bool bf16) { return N * (bf16 ? 2 : 4) % 16 == 0; }
+int pieces_of(int64_t N, bool bf16, bool vec) { return (int)(vec ? N * (bf16 ? 2 : 4) / 16 : N); }
+
+template <class Go>
+hipError_t on_type(bool bf16, bool vec, Go go) {
+  using Yes = std::true_type;
+  using No = std::false_type;
+  if (bf16) return vec ? go(Yes{}, Yes{}) : go(Yes{}, No{});
+  return vec ? go(No{}, Yes{}) : go(No{}, No{});
+}
+
+}  // namespace
+
+hipError_t launch_expert_gather(const void *x, bool bf16, int64_t T, int64_t N,
+                                const int32_t *rows, int64_t P, void *out, hipStream_t stream) {
+  const bool vec = whole_pieces(N, bf16);
+  const int pieces = pieces_of(N, bf16, vec);
+  const int parts = (pieces + 64 * kPieces - 1) / (64 * kPieces);
+  const unsigned groups = (unsigned)((P * parts + kWaves - 1) / kWaves);
+  return on_type(bf16, vec, [&](auto b, auto v) {
+    expert_gather_kernel<decltype(b)::value, decltype(v)::value>
+        <<<groups, kThreads, 0, stream>>>(x, T, pieces, rows, P, parts, out);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_expert_combine(const void *z, bool bf16, int64_t P, int64_t N,
+                                 const int32_t *slots, const float *weights, int64_t T, int k,
+                                 void *out, hipStream_t stream) {
+  const bool vec = whole_pieces(N, bf16);
+  const int pieces = pieces_of(N, bf16, vec);
+  const int parts = (pieces + 63) / 64;
+  const unsigned groups = (unsigned)((T * parts + kWaves - 1) / kWaves);
+  return on_type(bf16, vec, [&](auto b, auto v) {
+    expert_combine_kernel<decltype(b)::value, decltype(v)::value>
+        <<<groups, kThreads, 0, stream>>>(z, P, pieces, slots, weights, T, k, parts, out);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_expert_combine_backward(const void *dout, const void *z, bool bf16, int64_t P,
+                                          int64_t N, const int32_t *rows, const int32_t *slots,
+                                          const float *weights, int64_t T, int k, void *dz,
+                                          float *dweights, hipStream_t stream) {
+  const bool vec = whole_pieces(N, bf16);
+  const int pieces = pieces_of(N, bf16, vec);
+  const unsigned groups = (unsigned)(T + (dz ? (P + 63) / 64 : 0));
+  return on_type(bf16, vec, [&](auto b, auto v) {
+    constexpr bool B = decltype(b)::value, V = decltype(v)::value;
+    auto kern = k <= 4 ? expert_combine_backward_kernel<B, V, 4>
+                       : (k <= 8 ? expert_combine_backward_kernel<B, V, 8>
+                                 : expert_combine_backward_kernel<B, V, 16>);
+    kern<<<groups, kThreads, 0, stream>>>(dout, z, P, pieces, rows, slots, weights, T, k, dz,
+                                          dweights);
+    return hipGetLastError();
+  });
+}
+
+}  // namespace rfq

@@ -39,6 +39,8 @@ EXPORTS = (
     "rfq_gemm_split_noalloc", "rfq_hif4_gemm_split", "rfq_hif4_gemm_workspace_bytes",
     "rfq_block_assign", "rfq_block_release", "rfq_rope", "rfq_rope_backward", "rfq_kv_append",
     "rfq_kv_gather", "rfq_kv_attention", "rfq_kv_attention_workspace_bytes",
+    "rfq_route", "rfq_route_backward", "rfq_expert_sort", "rfq_expert_sort_workspace_bytes",
+    "rfq_expert_gather", "rfq_expert_combine", "rfq_expert_combine_backward", "rfq_gemm_experts",
     "rfq_status_str", "rfq_abi_version",
 )
 
@@ -141,13 +143,24 @@ def _load():
                                      I32, I64, H, P, P, I64, P]
     lib.rfq_kv_attention_workspace_bytes.argtypes = [I64] * 7
     lib.rfq_kv_attention_workspace_bytes.restype = I64
+    lib.rfq_route.argtypes = [P, I32, I64, I64, I64, I32, P, P, P]
+    lib.rfq_route_backward.argtypes = [P, P, I32, I64, I64, I64, P, P, I32, P, P]
+    lib.rfq_expert_sort.argtypes = [P, I64, I64, I64, I64, P, P, P, P, I64, P]
+    lib.rfq_expert_sort_workspace_bytes.argtypes = [I64] * 3
+    lib.rfq_expert_sort_workspace_bytes.restype = I64
+    lib.rfq_expert_gather.argtypes = [P, I32, I64, I64, P, I64, P, P]
+    lib.rfq_expert_combine.argtypes = [P, I32, I64, I64, P, P, I64, I64, P, P]
+    lib.rfq_expert_combine_backward.argtypes = [P, P, I32, I64, I64, P, P, P, I64, I64, P, P, P]
+    lib.rfq_gemm_experts.argtypes = [P] * 8 + [I64] * 5 + [P, I32, P]
     for f in ("rfq_quantize_act", "rfq_quantize_weight", "rfq_gemm", "rfq_dequant",
               "rfq_swiglu_quantize_act", "rfq_gemm_swiglu_quantize", "rfq_gemm_phi",
               "rfq_fallback_map", "rfq_gemm_stream", "rfq_hif4_quantize", "rfq_hif4_dequant",
               "rfq_hif4_gemm", "rfq_hif4_gemm_wbf16", "rfq_mfma_fp4_loop", "rfq_mfma_bf16_loop",
               "rfq_gemm_split", "rfq_hif4_gemm_split",
               "rfq_gemm_split_noalloc", "rfq_block_assign", "rfq_block_release", "rfq_rope",
-              "rfq_rope_backward", "rfq_kv_append", "rfq_kv_gather", "rfq_kv_attention"):
+              "rfq_rope_backward", "rfq_kv_append", "rfq_kv_gather", "rfq_kv_attention",
+              "rfq_route", "rfq_route_backward", "rfq_expert_sort", "rfq_expert_gather",
+              "rfq_expert_combine", "rfq_expert_combine_backward", "rfq_gemm_experts"):
         getattr(lib, f).restype = I32
     _bind_calls(lib)
     lib.rfq_status_str.argtypes = [I32]

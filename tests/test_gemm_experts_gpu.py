@@ -1,0 +1,200 @@
+"""The product with a weight matrix per expert against 64 bits: lengths of an expert from
+none to many, odd sizes, row maps, plain and with the residual, both output types; rows of
+no expert are left as they were."""
+import pytest
+import torch
+
+import experts_util as ref
+import paper_2608_26581_amd as rfq
+from gpu_util import TOL_BF16, TOL_SUM
+
+pytestmark = pytest.mark.gpu
+
+MARK = 12345.0
+
+
+def ints(values):
+    return torch.tensor(values, dtype=torch.int32).cuda()
+
+
+def starts(lengths, first=0):
+    out = [first]
+    for n in lengths:
+        out.append(out[-1] + n)
+    return out
+
+
+def check(a, w, offsets, rows, dtype, stream=None):
+    M = a[0].shape[0]
+    P = M if rows is None else rows.numel()
+    N = w[0].shape[1]
+    out = torch.full((P, N), MARK, dtype=dtype, device="cuda")
+    z = rfq.rfq_gemm_experts(*a, *w, offsets, rows=rows, out=out, stream=stream)
+    assert z is out
+    if stream is not None:
+        torch.cuda.current_stream().wait_stream(stream)
+    want, bound, live = ref.product(a, w, offsets, rows, M)
+    z = z.double().cpu()
+    assert (z[~live] == torch.tensor(MARK, dtype=dtype).double()).all()
+    err = (z - want).abs()[live]
+    tol = TOL_SUM * bound + (TOL_BF16 * want.abs() if dtype == torch.bfloat16 else 0.0)
+    assert (err <= tol[live]).all(), float((err - tol[live]).max())
+
+
+# Lengths of the experts, and the sizes N and K.
+LENGTHS = [
+    ([1], 16, 32), ([3, 0, 1], 17, 64), ([0, 0, 5, 0], 33, 96), ([16, 17, 1, 15], 64, 128),
+    ([0, 40, 0, 0, 25], 100, 160), ([2] * 9, 1, 512), ([1] * 70, 48, 544), ([64, 65, 63], 130, 1024),
+    ([7, 129, 128, 1, 0, 200], 256, 512), ([300, 5], 200, 320), ([0, 513, 257], 260, 768),
+    ([33] * 5, 96, 4128),
+]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("residual", [True, False])
+@pytest.mark.parametrize("mapped", [True, False])
+@pytest.mark.parametrize("lengths,N,K", LENGTHS)
+def test_product(lengths, N, K, mapped, residual, dtype):
+    P, E = sum(lengths), len(lengths)
+    M = max(1, P // 2) if mapped else P
+    a = ref.codes((M,), K, P + N, residual)
+    w = ref.codes((E, N), K, N, None)
+    rows = None
+    if mapped:
+        rows = torch.randint(0, M, (P,), generator=torch.Generator().manual_seed(P), dtype=torch.int32).cuda()
+    check(a, w, ints(starts(lengths)), rows, dtype)
+
+
+def test_rows_behind_the_last_and_before_the_first_are_left():
+    K, N = 128, 40
+    w = ref.codes((3, N), K, 1, None)
+    a = ref.codes((90,), K, 2)
+    check(a, w, ints([5, 20, 20, 61]), None, torch.bfloat16)
+    check(a, w, ints([0, 0, 0, 0]), None, torch.float32)
+    check(a, w, ints([90, 90, 90, 90]), None, torch.float32)
+
+
+def test_offsets_are_cut_to_the_slots():
+    K, N = 64, 33
+    w = ref.codes((3, N), K, 1, None)
+    a = ref.codes((50,), K, 2)
+    check(a, w, ints([-7, 20, 45, 99]), None, torch.float32)
+    check(a, w, ints([-2 ** 31, -5, 2 ** 31 - 1, 2 ** 31 - 1]), None, torch.float32)
+
+
+def test_row_indices_outside_count_as_zeros():
+    K, N = 160, 70
+    w = ref.codes((2, N), K, 1, None)
+    a = ref.codes((6,), K, 2)
+    rows = ints([0, -1, 6, 5, 2 ** 31 - 1, -2 ** 31, 3, 3, 1] + [4] * 30 + [-1] * 31)
+    check(a, w, ints([0, 8, 70]), rows, torch.float32)
+    check(a, w, ints([0, 8, 70]), rows, torch.bfloat16)
+
+
+def test_nan_reaches_only_its_own_row_and_column():
+    K, N = 256, 48
+    w = ref.codes((2, N), K, 1, None)
+    a = ref.codes((40,), K, 2)
+    off = ints([0, 18, 40])
+    clean = rfq.rfq_gemm_experts(*a, *w, off)
+    a[1][7, 3] = 255                                  # an activation row
+    w[1][1, 11, 2] = 255                              # a column of expert 1
+    z = rfq.rfq_gemm_experts(*a, *w, off)
+    bad = torch.zeros_like(z, dtype=torch.bool)
+    bad[7] = True
+    bad[18:, 11] = True
+    assert torch.isnan(z[bad]).all() and torch.equal(z[~bad], clean[~bad])
+
+
+def test_neighbours_past_k_have_no_influence():
+    """Scale bytes 0xFF right behind a row's end, in the next row, expert and tensor."""
+    K, N = 96, 20
+    w = ref.codes((2, N), K, 1, None)
+    a = ref.codes((20,), K, 2)
+    off = ints([0, 20, 20])
+    want = rfq.rfq_gemm_experts(*a, *w, off)
+    w[1][1] = 255
+    a[1][5] = 255
+    z = rfq.rfq_gemm_experts(*a, *w, off)
+    keep = torch.arange(20) != 5
+    assert torch.equal(z[keep.cuda()], want[keep.cuda()])
+
+
+def test_equal_to_the_dense_product_of_each_expert():
+    lengths, N, K = [200, 64, 300], 384, 1024
+    off = starts(lengths)
+    a = ref.codes((off[-1],), K, 3)
+    w = ref.codes((3, N), K, 4, None)
+    z = rfq.rfq_gemm_experts(*a, *w, ints(off)).double()
+    for e in range(3):
+        i, j = off[e], off[e + 1]
+        part = [t[i:j].contiguous() for t in a]
+        d = rfq.rfq_gemm(*part, w[0][e], w[1][e]).double()
+        _, bound, _ = ref.product(part, (w[0][e:e + 1], w[1][e:e + 1]), ints([0, j - i]), None, j - i)
+        assert ((z[i:j] - d).abs().cpu() <= 2 * TOL_SUM * bound).all()
+
+
+def test_same_bits_from_call_to_call_and_replay():
+    lengths, N, K = [150, 3, 0, 70, 20], 200, 2048
+    off = ints(starts(lengths))
+    a = ref.codes((sum(lengths),), K, 5)
+    w = ref.codes((5, N), K, 6, None)
+    out = torch.full((sum(lengths), N), MARK, device="cuda")
+    rfq.rfq_gemm_experts(*a, *w, off, out=out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        z = rfq.rfq_gemm_experts(*a, *w, off)
+    for other in ([150, 3, 0, 70, 20], [0, 0, 243, 0, 0], [10, 1, 100, 2, 0]):
+        off.copy_(ints(starts(other)))
+        z.fill_(MARK)
+        graph.replay()
+        want = torch.full_like(out, MARK)
+        rfq.rfq_gemm_experts(*a, *w, off, out=want)
+        torch.cuda.synchronize()
+        assert torch.equal(z, want)
+
+
+def test_on_another_stream():
+    a, w = ref.codes((60,), 256, 1), ref.codes((4, 64), 256, 2, None)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    check(a, w, ints([0, 10, 30, 31, 60]), None, torch.bfloat16, stream=s)
+
+
+def test_more_than_64_experts_and_the_most():
+    for E in (65, 200, 1024):
+        g = torch.Generator().manual_seed(E)
+        lengths = torch.randint(0, 4, (E,), generator=g).tolist()
+        P = sum(lengths)
+        a, w = ref.codes((P,), 64, 1), ref.codes((E, 24), 64, 2, None)
+        check(a, w, ints(starts(lengths)), None, torch.float32)
+
+
+def test_empty_and_refusals():
+    a, w = ref.codes((8,), 64, 1), ref.codes((2, 32), 64, 2, None)
+    off = ints([0, 3, 8])
+    none = [t[:0] if t is not None else None for t in a]
+    assert rfq.rfq_gemm_experts(*none, *w, ints([0, 0, 0])).shape == (0, 32)
+    assert rfq.rfq_gemm_experts(*a, w[0][:, :0].contiguous(), w[1][:, :0].contiguous(), off).shape == (8, 0)
+    z = rfq.rfq_gemm_experts(*none, *w, off, rows=ints([0] * 8))     # no activations: zeros
+    assert (z == 0).all()
+    with pytest.raises(ValueError, match="3-D"):
+        rfq.rfq_gemm_experts(*a, w[0][0], w[1][0], off)
+    with pytest.raises(ValueError, match="offsets"):
+        rfq.rfq_gemm_experts(*a, *w, off[:2])
+    with pytest.raises(ValueError, match="w scales"):
+        rfq.rfq_gemm_experts(*a, w[0], w[1][:1], off)
+    with pytest.raises(ValueError, match="both"):
+        rfq.rfq_gemm_experts(a[0], a[1], a[2], None, *w, off)
+    with pytest.raises(ValueError, match="w codes"):
+        rfq.rfq_gemm_experts(*ref.codes((8,), 128, 1), *w, off)
+    with pytest.raises(ValueError, match="1-D"):
+        rfq.rfq_gemm_experts(*a, *w, off, rows=ints([[0] * 8]))
+    with pytest.raises(TypeError):
+        rfq.rfq_gemm_experts(*a, *w, off.long())
+    with pytest.raises(TypeError, match="out_dtype"):
+        rfq.rfq_gemm_experts(*a, *w, off, out_dtype=torch.float16)
+    big = ref.codes((1025, 16), 32, 2, None)
+    with pytest.raises(rfq.RfqError, match="RFQ_ERR_SHAPE"):
+        rfq.rfq_gemm_experts(*ref.codes((8,), 32, 1), *big, ints([0] * 1026))
