@@ -745,7 +745,7 @@ rfq_status rfq_expert_combine_backward(const void *dout, const void *z, rfq_dtyp
  *   z       [P][N] row-major, z_dtype.
  * Codes, scales and z are 16-byte aligned.  The codes of the activations and those of one
  * expert stay below 2 GiB each; M, P + 256 and N + 256 below 2^31; min(P, P / 16 + E) *
- * ceil(N / 16) below 2^31 - 2^20.
+ * ceil(N / 32) at most 2^24 - 9.
  */
 rfq_status rfq_gemm_experts(const uint8_t *q_codes, const uint8_t *q_scales,
                             const uint8_t *r_codes, const uint8_t *r_scales,
