@@ -56,6 +56,18 @@ struct KvLib {
   decltype(&rfq_kv_attention_workspace_bytes) kv_attention_workspace_bytes;
 } kv;
 
+// Entry points of the calls around a layer of experts (bind_experts()).
+struct ExpertsLib {
+  decltype(&rfq_route) route;
+  decltype(&rfq_route_backward) route_backward;
+  decltype(&rfq_expert_sort) expert_sort;
+  decltype(&rfq_expert_sort_workspace_bytes) expert_sort_workspace_bytes;
+  decltype(&rfq_expert_gather) expert_gather;
+  decltype(&rfq_expert_combine) expert_combine;
+  decltype(&rfq_expert_combine_backward) expert_combine_backward;
+  decltype(&rfq_gemm_experts) gemm_experts;
+} ex;
+
 // A plain torch.Tensor (no subclass), contiguous, strided, 2-D, on device dev.
 const at::Tensor *plain(PyObject *o, int dev) {
   if (!THPVariable_CheckExact(o)) return nullptr;
@@ -673,7 +685,256 @@ PyObject *kv_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// bind(addresses), bind_kv(addresses): the entry points, in Lib's and KvLib's order.
+// ---- the calls around a layer of experts
+
+// Parts of one allocation of 4-byte elements, each on 256 bytes (two take about 1 us of the
+// host's time more than one).
+struct Part { at::IntArrayRef sizes; at::ScalarType type; };
+template <size_t N>
+void parts(const at::Tensor &like, const Part (&p)[N], at::Tensor (&t)[N]) {
+  int64_t total = 0, at = 0, n[N];
+  for (size_t i = 0; i < N; ++i) {
+    n[i] = 1;
+    for (int64_t s : p[i].sizes) n[i] *= s;
+    total += (n[i] + 63) / 64 * 64;
+  }
+  const NoGil unlocked;
+  const at::Tensor all = empty(like, {total}, at::kInt);
+  for (size_t i = 0; i < N; ++i) {
+    t[i] = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(all.storage()), all.key_set(),
+                                                    c10::scalarTypeToTypeMeta(p[i].type));
+    t[i].unsafeGetTensorImpl()->set_sizes_contiguous(p[i].sizes);
+    t[i].unsafeGetTensorImpl()->set_storage_offset(at);
+    at += (n[i] + 63) / 64 * 64;
+  }
+}
+
+const int32_t *int_data(const at::Tensor *t) { return static_cast<const int32_t *>(t->data_ptr()); }
+const float *float_data(const at::Tensor *t) {
+  return t ? static_cast<const float *>(t->data_ptr()) : nullptr;
+}
+
+// [rows][cols] of fp32 or bf16.
+const at::Tensor *matrix(PyObject *o, int dev) {
+  const at::Tensor *t = plain(o, dev);
+  return t && float_code(*t) >= 0 ? t : nullptr;
+}
+
+// A plan's tensors: rows [T k] and slots [T][k] (the offsets have only to be ints).
+struct Plan { const at::Tensor *rows, *slots; int64_t T, k; };
+bool plan_of(PyObject *const *a, int dev, Plan &p) {
+  if (!THPVariable_CheckExact(a[0]) || THPVariable_Unpack(a[0]).dim() != 1 ||
+      !vector(a[0], dev, THPVariable_Unpack(a[0]).size(0)))
+    return false;
+  p.slots = ints(a[2], dev);
+  if (!p.slots) return false;
+  p.T = p.slots->size(0);
+  p.k = p.slots->size(1);
+  p.rows = vector(a[1], dev, p.T * p.k);
+  return p.rows != nullptr;
+}
+
+// route(logits, k, renormalize) -> (weights, experts).
+PyObject *route(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  const int dev = n != 3 ? -1 : device_for(a[0]);
+  int64_t k;
+  if (dev < 0 || !integer(a[1], k) || k < 1 || k > 16) return none();
+  const at::Tensor *l = matrix(a[0], dev);
+  const int renormalize = PyObject_IsTrue(a[2]);
+  if (renormalize < 0) return nullptr;
+  if (!l || k > l->size(1)) return none();
+  const int64_t T = l->size(0), E = l->size(1);
+  at::Tensor t[2];
+  parts(*l, {{{T, k}, at::kFloat}, {{T, k}, at::kInt}}, t);
+  const int st = call(ex.route, l->data_ptr(), float_code(*l), T, E, k, renormalize,
+                      static_cast<float *>(t[0].data_ptr()),
+                      static_cast<int32_t *>(t[1].data_ptr()), stream_of(dev));
+  return st ? failed(st) : tuple(t, 2);
+  END_HANDLE_TH_ERRORS
+}
+
+// route_backward(dweights, logits, weights, experts, renormalize) -> dlogits.
+PyObject *route_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  const int dev = n != 5 ? -1 : device_for(a[1]);
+  if (dev < 0) return none();
+  const at::Tensor *l = matrix(a[1], dev), *w = plain(a[2], dev);
+  const int renormalize = PyObject_IsTrue(a[4]);
+  if (renormalize < 0) return nullptr;
+  if (!l || !w) return none();
+  const int64_t T = l->size(0), E = l->size(1), k = w->size(1);
+  const at::Tensor *d = plain(a[0], dev), *x = plain(a[3], dev);
+  if (!is(w, at::kFloat, T, k) || !is(d, at::kFloat, T, k) || !is(x, at::kInt, T, k)) return none();
+  at::Tensor out;
+  {
+    const NoGil unlocked;
+    out = empty(*l, {T, E}, l->scalar_type());
+  }
+  const int st = call(ex.route_backward, float_data(d), l->data_ptr(), float_code(*l), T, E, k,
+                      float_data(w), int_data(x), renormalize, out.data_ptr(), stream_of(dev));
+  return st ? failed(st) : THPVariable_Wrap(out);
+  END_HANDLE_TH_ERRORS
+}
+
+// expert_sort(experts, E, first, workspace or None) -> (offsets, rows, slots).
+PyObject *expert_sort(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  const int dev = n != 4 ? -1 : device_for(a[0]);
+  int64_t E, first;
+  if (dev < 0 || !integer(a[1], E) || !integer(a[2], first) || E < 1 || E > 1024) return none();
+  const at::Tensor *x = ints(a[0], dev);
+  if (!x) return none();
+  const int64_t T = x->size(0), k = x->size(1);
+  at::Tensor t[3], work;
+  int64_t bytes;
+  if (a[3] == Py_None) {
+    bytes = ex.expert_sort_workspace_bytes(T, k, E);
+    if (bytes > 0) {
+      const NoGil unlocked;
+      work = empty(*x, {bytes}, at::kByte);
+    }
+  } else {
+    if (!THPVariable_CheckExact(a[3])) return none();
+    const at::Tensor &w = THPVariable_Unpack(a[3]);
+    if (!w.is_cuda() || w.layout() != at::kStrided || !w.is_contiguous() ||
+        w.get_device() != dev || w.scalar_type() != at::kByte)
+      return none();
+    work = w;
+    bytes = w.numel();
+  }
+  parts(*x, {{{E + 1}, at::kInt}, {{T * k}, at::kInt}, {{T, k}, at::kInt}}, t);
+  auto p = [](const at::Tensor &y) { return static_cast<int32_t *>(y.data_ptr()); };
+  const int st = call(ex.expert_sort, int_data(x), T, k, first, E, p(t[0]), p(t[1]), p(t[2]),
+                      work.defined() ? work.data_ptr() : nullptr, bytes, stream_of(dev));
+  return st ? failed(st) : tuple(t, 3);
+  END_HANDLE_TH_ERRORS
+}
+
+// out (given, of like's type) or a new [rows][cols] tensor; undefined where it does not fit.
+at::Tensor rows_out(PyObject *out, const at::Tensor &like, int64_t rows, int64_t cols, int dev) {
+  if (out != Py_None) {
+    const at::Tensor *t = plain(out, dev);
+    return is(t, like.scalar_type(), rows, cols) ? *t : at::Tensor();
+  }
+  const NoGil unlocked;
+  return empty(like, {rows, cols}, like.scalar_type());
+}
+
+// expert_gather(x, offsets, rows, slots, out) -> xs.
+PyObject *expert_gather(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  const int dev = n != 5 ? -1 : device_for(a[0]);
+  Plan p;
+  if (dev < 0 || !plan_of(a + 1, dev, p)) return none();
+  const at::Tensor *x = matrix(a[0], dev);
+  if (!x || x->size(0) != p.T) return none();
+  const int64_t N = x->size(1), P = p.T * p.k;
+  const at::Tensor y = rows_out(a[4], *x, P, N, dev);
+  if (!y.defined()) return none();
+  const int st = call(ex.expert_gather, x->data_ptr(), float_code(*x), p.T, N, int_data(p.rows), P,
+                      y.data_ptr(), stream_of(dev));
+  return st ? failed(st) : result(a[4], y);
+  END_HANDLE_TH_ERRORS
+}
+
+// [T][k] fp32 weights or None.
+bool weights_of(PyObject *o, int dev, const Plan &p, const at::Tensor *&w) {
+  w = nullptr;
+  if (o == Py_None) return true;
+  w = plain(o, dev);
+  return is(w, at::kFloat, p.T, p.k);
+}
+
+// expert_combine(z, weights or None, offsets, rows, slots, out) -> out.
+PyObject *expert_combine(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  const int dev = n != 6 ? -1 : device_for(a[0]);
+  Plan p;
+  const at::Tensor *w;
+  if (dev < 0 || !plan_of(a + 2, dev, p) || !weights_of(a[1], dev, p, w)) return none();
+  const at::Tensor *z = matrix(a[0], dev);
+  if (!z || z->size(0) != p.T * p.k) return none();
+  const int64_t N = z->size(1);
+  const at::Tensor y = rows_out(a[5], *z, p.T, N, dev);
+  if (!y.defined()) return none();
+  const int st = call(ex.expert_combine, z->data_ptr(), float_code(*z), p.T * p.k, N,
+                      int_data(p.slots), float_data(w), p.T, p.k, y.data_ptr(), stream_of(dev));
+  return st ? failed(st) : result(a[5], y);
+  END_HANDLE_TH_ERRORS
+}
+
+// expert_combine_backward(dout, z, weights or None, offsets, rows, slots) -> (dz, dweights).
+PyObject *expert_combine_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  const int dev = n != 6 ? -1 : device_for(a[1]);
+  Plan p;
+  const at::Tensor *w;
+  if (dev < 0 || !plan_of(a + 3, dev, p) || !weights_of(a[2], dev, p, w)) return none();
+  const at::Tensor *z = matrix(a[1], dev), *d = plain(a[0], dev);
+  if (!z || z->size(0) != p.T * p.k || !is(d, z->scalar_type(), p.T, z->size(1))) return none();
+  const int64_t P = p.T * p.k, N = z->size(1);
+  at::Tensor t[2];
+  {
+    const NoGil unlocked;
+    t[0] = empty(*z, {P, N}, z->scalar_type());
+    t[1] = empty(*z, {p.T, p.k}, at::kFloat);
+  }
+  const int st = call(ex.expert_combine_backward, d->data_ptr(), z->data_ptr(), float_code(*z), P, N,
+                      int_data(p.rows), int_data(p.slots), float_data(w), p.T, p.k, t[0].data_ptr(),
+                      static_cast<float *>(t[1].data_ptr()), stream_of(dev));
+  return st ? failed(st) : tuple(t, 2);
+  END_HANDLE_TH_ERRORS
+}
+
+// gemm_experts(q, qs, r or None, rs, w, ws, offsets, rows or None, dtype code, out) -> Z.
+PyObject *gemm_experts(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  const int dev = n != 10 ? -1 : device_for(a[0]);
+  int64_t code;
+  if (dev < 0 || !integer(a[8], code)) return none();
+  const at::Tensor *qc = plain(a[0], dev);
+  if (!qc || qc->scalar_type() != at::kByte) return none();
+  const int64_t M = qc->size(0), K = qc->size(1) * 2;
+  Operand q, r;
+  if (!operand<false>(a[0], a[1], M, K, dev, q) ||
+      !(a[2] == Py_None ? a[3] == Py_None : operand<false>(a[2], a[3], M, K, dev, r)))
+    return none();
+  auto cube = [&](PyObject *o) -> const at::Tensor * {
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    return t.is_cuda() && t.layout() == at::kStrided && t.dim() == 3 && t.is_contiguous() &&
+                   t.get_device() == dev && t.scalar_type() == at::kByte
+               ? &t
+               : nullptr;
+  };
+  const at::Tensor *wc = cube(a[4]), *ws = cube(a[5]);
+  if (!wc || !ws) return none();
+  const int64_t E = wc->size(0), N = wc->size(1);
+  if (wc->size(2) != K / 2 || ws->size(0) != E || ws->size(1) != N || ws->size(2) != K / 32)
+    return none();
+  const at::Tensor *off = vector(a[6], dev, E + 1), *rows = nullptr;
+  if (!off) return none();
+  int64_t P = M;
+  if (a[7] != Py_None) {
+    if (!THPVariable_CheckExact(a[7]) || THPVariable_Unpack(a[7]).dim() != 1) return none();
+    P = THPVariable_Unpack(a[7]).size(0);
+    rows = vector(a[7], dev, P);
+    if (!rows) return none();
+  }
+  const at::Tensor z = output(a[9], (int)code, *qc, P, N, dev);
+  if (!z.defined()) return none();
+  auto u8 = [](const void *p) { return static_cast<const uint8_t *>(p); };
+  const int st = call(ex.gemm_experts, u8(q.c()), u8(q.s()), u8(r.c()), u8(r.s()),
+                      u8(wc->data_ptr()), u8(ws->data_ptr()), int_data(off),
+                      rows ? int_data(rows) : nullptr, M, P, E, N, K, z.data_ptr(), float_code(z),
+                      stream_of(dev));
+  return st ? failed(st) : result(a[9], z);
+  END_HANDLE_TH_ERRORS
+}
+
+// bind(addresses), bind_kv(addresses), bind_experts(addresses): the entry points, in the
+// order of Lib, KvLib and ExpertsLib.
 template <class L>
 PyObject *bind_to(L &to, PyObject *const *a, Py_ssize_t n) {
   void **slot = reinterpret_cast<void **>(&to);
@@ -693,6 +954,7 @@ PyObject *bind_to(L &to, PyObject *const *a, Py_ssize_t n) {
 }
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) { return bind_to(lib, a, n); }
 PyObject *bind_kv(PyObject *, PyObject *const *a, Py_ssize_t n) { return bind_to(kv, a, n); }
+PyObject *bind_experts(PyObject *, PyObject *const *a, Py_ssize_t n) { return bind_to(ex, a, n); }
 
 #define RFQ_METHOD(name, fn) \
   {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fn)), METH_FASTCALL, nullptr}
@@ -713,6 +975,14 @@ PyMethodDef methods[] = {RFQ_METHOD("bind", bind),
                          RFQ_METHOD("kv_append", kv_append),
                          RFQ_METHOD("kv_gather", kv_gather),
                          RFQ_METHOD("kv_attention", kv_attention),
+                         RFQ_METHOD("bind_experts", bind_experts),
+                         RFQ_METHOD("route", route),
+                         RFQ_METHOD("route_backward", route_backward),
+                         RFQ_METHOD("expert_sort", expert_sort),
+                         RFQ_METHOD("expert_gather", expert_gather),
+                         RFQ_METHOD("expert_combine", expert_combine),
+                         RFQ_METHOD("expert_combine_backward", expert_combine_backward),
+                         RFQ_METHOD("gemm_experts", gemm_experts),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rfq_calls", nullptr, -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

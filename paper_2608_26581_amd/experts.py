@@ -6,18 +6,47 @@ tensors as the other calls do.  A plan is an ExpertPlan, or any three tensors of
 layout.  The router's weights are differentiable in the logits, gather in x and
 combine in z and the weights; what goes through the 4-bit product is not.
 """
+import ctypes
+import threading
 from typing import NamedTuple
 
 import torch
 from torch.autograd.function import once_differentiable
 
+from . import rfq as _binding
 from .rfq import (
-    _FLOAT, _U8, _check, _dtype_code, _empty, _need, _need_pair, _ptr, _stream, _torch_stream,
-    _written, _z_out, load,
+    _FLOAT, _OUT_CODE, _U8, _check, _dtype_code, _empty, _need, _need_pair, _ptr, _result, _stream,
+    _torch_stream, _written, _z_out, load,
 )
 
 _I32 = (torch.int32,)
 _F32 = (torch.float32,)
+
+# The entry points that the native calls use here, in the order their bind_experts() takes,
+# and the module that has them.
+_NATIVE_ENTRIES = (
+    "rfq_route", "rfq_route_backward", "rfq_expert_sort", "rfq_expert_sort_workspace_bytes",
+    "rfq_expert_gather", "rfq_expert_combine", "rfq_expert_combine_backward", "rfq_gemm_experts",
+)
+_bound = None
+_bind_lock = threading.Lock()
+
+
+def _native(func, *args):
+    """The result of a native call, or None where the Python path takes over."""
+    global _bound
+    calls = _binding._calls
+    if calls is None or _bound is not calls:
+        lib = load()
+        calls = _binding._calls
+        if not calls:
+            return None
+        with _bind_lock:
+            if _bound is not calls:
+                calls.bind_experts(*(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value
+                                     for f in _NATIVE_ENTRIES))
+                _bound = calls
+    return _result(func, getattr(calls, func)(*args))
 
 
 class ExpertPlan(NamedTuple):
@@ -87,6 +116,10 @@ class _Route(torch.autograd.Function):
 
 
 def _route(logits, k, renormalize, stream):
+    if stream is None:
+        r = _native("route", logits, k, renormalize)
+        if r is not None:
+            return r
     _need_2d(logits, "logits", _FLOAT)
     dev, (T, E) = logits.get_device(), logits.shape
     k = int(k)
@@ -113,6 +146,10 @@ def rfq_route(logits, k, renormalize=True, stream=None):
 def rfq_route_backward(dweights, logits, weights, experts, renormalize=True, stream=None):
     """The gradient [T][E] (dtype of logits) of rfq_route(logits, k) -> weights, experts from
     that of its weights."""
+    if stream is None:
+        r = _native("route_backward", dweights, logits, weights, experts, renormalize)
+        if r is not None:
+            return r
     _need_2d(logits, "logits", _FLOAT)
     dev, (T, E) = logits.get_device(), logits.shape
     _need_2d(weights, "weights", _F32, dev)
@@ -139,7 +176,11 @@ def rfq_expert_sort(experts, n_experts, first=0, workspace=None, stream=None):
     """The pairs of experts [T][k] sorted by expert, those of an expert in their order ->
     ExpertPlan.  Experts outside [first, first + n_experts) are dropped.  workspace: a
     contiguous uint8 tensor of rfq_expert_sort_workspace_bytes, or None: one from torch's
-    allocator."""
+    allocator.  The three may be parts of one allocation."""
+    if stream is None:
+        r = _native("expert_sort", experts, n_experts, first, workspace)
+        if r is not None:
+            return ExpertPlan(*r)
     _need_2d(experts, "experts", _I32)
     dev, (T, k) = experts.get_device(), experts.shape
     E = int(n_experts)
@@ -174,6 +215,10 @@ class _Gather(torch.autograd.Function):
 
 
 def _gather(x, plan, out, stream):
+    if stream is None:
+        r = _native("expert_gather", x, *plan, out)
+        if r is not None:
+            return r if out is None else _written(out)
     _need_2d(x, "x", _FLOAT)
     dev, (T, N) = x.get_device(), x.shape
     rows, slots = _need_plan(plan, dev)
@@ -229,6 +274,10 @@ class _Sum(torch.autograd.Function):
 
 
 def _combine(z, weights, plan, out, stream):
+    if stream is None:
+        r = _native("expert_combine", z, weights, *plan, out)
+        if r is not None:
+            return r if out is None else _written(out)
     _need_2d(z, "z", _FLOAT)
     dev, (P, N) = z.get_device(), z.shape
     rows, slots = _need_plan(plan, dev)
@@ -262,6 +311,10 @@ def rfq_expert_combine(z, weights, plan, out=None, stream=None):
 
 
 def _combine_backward(dout, z, weights, plan, need_z, need_w, stream):
+    if stream is None and need_z and need_w:
+        r = _native("expert_combine_backward", dout, z, weights, *plan)
+        if r is not None:
+            return r
     _need_2d(z, "z", _FLOAT)
     dev, (P, N) = z.get_device(), z.shape
     rows, slots = _need_plan(plan, dev)
@@ -294,6 +347,11 @@ def rfq_gemm_experts(q_codes, q_scales, r_codes, r_scales, w_codes, w_scales, of
     (rows None: row s) times w_codes [E][N][K/2], w_scales [E][N][K/32]; r_* None gives plain
     MXFP4.  Rows of Z that belong to no expert are not written; a row index outside the
     activations counts as a row of zeros."""
+    if stream is None:
+        r = _native("gemm_experts", q_codes, q_scales, r_codes, r_scales, w_codes, w_scales, offsets,
+                    rows, _OUT_CODE.get(out_dtype, 2), out)
+        if r is not None:
+            return r if out is None else _written(out)
     _need_2d(q_codes, "q codes", _U8)
     dev, M, K = q_codes.get_device(), q_codes.shape[0], 2 * q_codes.shape[1]
     _need(q_scales, "q scales", _U8, (M, K // 32), dev)
