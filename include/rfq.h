@@ -744,8 +744,8 @@ rfq_status rfq_expert_combine_backward(const void *dout, const void *z, rfq_dtyp
  *   offsets [E + 1], not decreasing and cut to [0, P];  rows [P] or NULL (then P == M).
  *   z       [P][N] row-major, z_dtype.
  * Codes, scales and z are 16-byte aligned.  The codes of the activations and those of one
- * expert stay below 2 GiB each; M, P + 256 and N + 256 below 2^31; min(P, P / 16 + E) *
- * ceil(N / 32) at most 2^24 - 9.
+ * expert stay below 2 GiB each; M, P + 256 and N + 256 below 2^31; (P / 128 + 2 E) *
+ * ceil(N / 64) at most 2^24 - 16.
  */
 rfq_status rfq_gemm_experts(const uint8_t *q_codes, const uint8_t *q_scales,
                             const uint8_t *r_codes, const uint8_t *r_scales,

@@ -14,8 +14,8 @@ struct ExpertTiles {
   int E, P, above, most;
 };
 
-// A tile's expert and first slot; end: the expert's.
-struct RowTile { int e, s0, end; };
+// A tile's expert, first slot and column tile; end: the expert's.
+struct RowTile { int e, s0, end, tn; };
 
 namespace {
 
@@ -32,25 +32,36 @@ __device__ __forceinline__ int wave_inclusive_sum(int v) {
 }
 
 struct Slots { int begin, end; };
-__device__ __forceinline__ Slots expert_slots(const ExpertTiles &x, int e) {
-  const int b = min(max(x.offsets[e], 0), x.P), c = min(max(x.offsets[e + 1], b), x.P);
+// The slots between two offsets, none where they are another launch's.
+__device__ __forceinline__ Slots slots_between(const ExpertTiles &x, int from, int to) {
+  const int b = min(max(from, 0), x.P), c = min(max(to, b), x.P);
   return {b, c - b > x.above && c - b <= x.most ? c : b};
 }
 
 // The experts' row tiles of kRows slots counted by a wave, each lane having the same number
-// of consecutive experts.
+// of consecutive experts: up to kHeld of them (256 experts) with their offsets in registers,
+// which a workgroup then finds its tile in after one round trip to memory.
 template <int kRows>
 struct TileCount {
-  int per, mine, incl, total;
+  static constexpr int kHeld = 4;
+  int per, mine, incl, total, held[kHeld + 1];
+  static __device__ __forceinline__ int tiles(const Slots &s) {
+    return (s.end - s.begin + kRows - 1) / kRows;
+  }
   __device__ __forceinline__ explicit TileCount(const ExpertTiles &x) {
     const int lane = threadIdx.x & 63;
     per = (x.E + 63) / 64;
+    const int e0 = min(lane * per, x.E);
     mine = 0;
-    for (int i = 0; i < per; ++i) {
-      const int e = lane * per + i;
-      if (e < x.E) {
-        const Slots s = expert_slots(x, e);
-        mine += (s.end - s.begin + kRows - 1) / kRows;
+#pragma unroll
+    for (int i = 0; i <= kHeld; ++i) held[i] = x.offsets[min(e0 + min(i, per), x.E)];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) mine += tiles(slots_between(x, held[i], held[i + 1]));
+    if (per > kHeld) {
+      mine = 0;
+      for (int i = 0; i < per; ++i) {
+        const int e = min(e0 + i, x.E);
+        mine += tiles(slots_between(x, x.offsets[e], x.offsets[min(e + 1, x.E)]));
       }
     }
     incl = wave_inclusive_sum(mine);
@@ -60,35 +71,50 @@ struct TileCount {
   __device__ __forceinline__ int find(const ExpertTiles &x, int t, Slots &s, int &first) const {
     const int l = __builtin_ctzll(__ballot(incl > t));
     first = __builtin_amdgcn_readlane(incl - mine, l);
-    for (int e = l * per, last = min(e + per, x.E); e < last; ++e) {
-      s = expert_slots(x, e);
-      const int tiles = (s.end - s.begin + kRows - 1) / kRows;
-      if (t < first + tiles) return e;
-      first += tiles;
+    int e = l * per;
+    if (per <= kHeld) {
+      int from = __builtin_amdgcn_readlane(held[0], l);
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) {
+        const int to = __builtin_amdgcn_readlane(held[i + 1], l);
+        s = slots_between(x, from, to);
+        const int n = tiles(s);
+        if (t < first + n) return e + i;
+        first += n;
+        from = to;
+      }
+      return -1;
+    }
+    for (const int last = min(e + per, x.E); e < last; ++e) {
+      s = slots_between(x, x.offsets[e], x.offsets[e + 1]);
+      const int n = tiles(s);
+      if (t < first + n) return e;
+      first += n;
     }
     return -1;
   }
 };
 
-// Tile blockIdx.x of the experts' tiles of kRows slots by ntn column tiles; false past the
-// last.  The tiles of one XCD (workgroups are dealt to the 8 XCDs round robin) are
-// consecutive, an expert's walked in groups of GM row tiles, so that the tiles that run
-// together share rows and weights in that XCD's L2.
-template <int kRows, int GM>
-__device__ __forceinline__ bool expert_tile(const ExpertTiles &x, int ntn, RowTile &tile, int &tn) {
+// Tile `bid` (a workgroup's number) of the experts' tiles of kRows slots by ntn column tiles;
+// false past the last.  An expert's tiles are walked in groups of GM row tiles, so that those
+// that run together share rows and weights.  SPREAD: workgroups are dealt to the 8 XCDs round
+// robin, and each XCD gets consecutive tiles, which share them in its L2 (half of 128 experts'
+// products for 8192 tokens, 256 x 256 tiles: 150 us without, 139 with it).
+template <int kRows, int GM, bool SPREAD>
+__device__ __forceinline__ bool expert_tile(const ExpertTiles &x, int bid, int ntn, RowTile &tile) {
   const TileCount<kRows> count(x);
   const int tiles = count.total * ntn, chunk = (tiles + 7) / 8;
-  const int t = (int)(blockIdx.x & 7) * chunk + (int)(blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= chunk || t >= tiles) return false;
+  const int t = SPREAD ? (bid & 7) * chunk + (bid >> 3) : bid;
+  if ((SPREAD && (bid >> 3) >= chunk) || t >= tiles) return false;
   Slots s;
   int first;
   if ((tile.e = count.find(x, t / ntn, s, first)) < 0) return false;
-  const int at = t - first * ntn, ntm = (s.end - s.begin + kRows - 1) / kRows;
+  const int at = t - first * ntn, ntm = TileCount<kRows>::tiles(s);
   const int group = at / (GM * ntn), size = min(ntm - group * GM, GM);
   const int in = at - group * GM * ntn;
   tile.s0 = s.begin + (group * GM + in % size) * kRows;
   tile.end = s.end;
-  tn = in / size;
+  tile.tn = in / size;
   return true;
 }
 

@@ -224,6 +224,15 @@ constexpr int kPhiRows = 64, kPhiK = 256;
 // LDS reserved for the map rows of a workgroup (K up to 2^20).
 constexpr int kPhiMapMaxBytes = Big::kWaveRows * ((1 << 20) / kPhiK);
 
+// EXPERTS: the wave's row of waves in the tile.  With two of them every second tile has them
+// swapped: the waves of a tile's lower half, which idle where an expert ends in its upper half,
+// would otherwise always be those of the same SIMDs.
+template <class C>
+__device__ __forceinline__ int expert_wave_row() {
+  const int wm = (int)(threadIdx.x >> 6) / C::kWaveCols;
+  return C::kWaveRows == 2 ? wm ^ ((int)(blockIdx.x >> 3) & 1) : wm;
+}
+
 // The product of one workgroup tile (both tile shapes; the kernels below
 // fix the shape and the occupancy).  SPLIT: the grid holds ceil(K / ksplit)
 // copies of the tile grid, copy s multiplying K columns [s ksplit, (s + 1)
@@ -238,16 +247,20 @@ constexpr int kPhiMapMaxBytes = Big::kWaveRows * ((1 << 20) / kPhiK);
 // shifted into place when a stage's word is written to LDS.
 //
 // EXPERTS: the rows are slots sorted by expert and the weights those of the slot's expert
-// (ExpertTiles); M is the number of activation rows.  A slot's row index is looked up once
-// per buffer row; one outside [0, M) loads zeros.  Code tensors are below 2 GiB.
+// (ExpertTiles, and the tile); M is the number of activation rows.  A slot's row index is
+// looked up once per buffer row; one outside [0, M) loads zeros.  Code tensors are below
+// 2 GiB.  IDLE: the wave's rows are all past the expert's end, so that it only moves its share
+// of the operands, with the barriers of the others.  (Two instances, chosen by the kernel: a
+// branch around the multiplications inside one makes the register allocator spill.)
 template <class C, bool RES, bool ZBF16, bool SWIGLU, bool HRES, bool PHI, bool SPLIT = false,
-          bool GK = false, bool EXPERTS = false>
+          bool GK = false, bool EXPERTS = false, bool IDLE = false>
 __device__ __forceinline__ void gemm_tile(
     const uint8_t *__restrict__ qc, const uint8_t *__restrict__ qs,
     const uint8_t *__restrict__ rc, const uint8_t *__restrict__ rs,
     const uint8_t *__restrict__ wc, const uint8_t *__restrict__ ws,
     int64_t M, int64_t N, int64_t K, void *__restrict__ z, const SwigluOut so,
-    const uint8_t *__restrict__ phi, int64_t ksplit, const ExpertTiles ex = ExpertTiles{}) {
+    const uint8_t *__restrict__ phi, int64_t ksplit, const ExpertTiles ex = ExpertTiles{},
+    const RowTile tile = RowTile{}) {
   static_assert(!PHI || C::kTM == kPhiRows, "a wave's rows are one indicator row");
   static_assert(!SPLIT || (!ZBF16 && !SWIGLU && !PHI), "split partials are fp32 products");
   static_assert(!EXPERTS || (!SPLIT && !SWIGLU && !PHI), "plain products by expert");
@@ -267,8 +280,7 @@ __device__ __forceinline__ void gemm_tile(
   int tm, tn;
   int64_t m0, mend = M;           // the tile's first row, and the end of the rows stored
   if constexpr (EXPERTS) {
-    RowTile tile;
-    if (!expert_tile<kBM, 1024 / kBM>(ex, ntn, tile, tn)) return;
+    tn = tile.tn;
     m0 = tile.s0;
     mend = tile.end;
     wc += (int64_t)tile.e * N * (K / 2);
@@ -287,7 +299,7 @@ __device__ __forceinline__ void gemm_tile(
 
   const int tid = threadIdx.x;
   const int lane = tid & 63, wave = tid >> 6;
-  const int wm = wave / C::kWaveCols, wn = wave % C::kWaveCols;
+  const int wm = EXPERTS ? expert_wave_row<C>() : wave / C::kWaveCols, wn = wave % C::kWaveCols;
   const int64_t kbytes = K / 2, kblocks = K / 32;
   // MX blocks of this workgroup's K range, and the stages that hold them.
   const int nblocks = (int)((SPLIT ? min(ksplit, K - kb) : K) / 32);
@@ -564,6 +576,22 @@ __device__ __forceinline__ void gemm_tile(
       on = (phi_word(st) >> (8 * wm_u)) & 0xFFu;
       if constexpr (HANDOVER) lmask = res_mask(min(st + 1 + D, last));
     }
+    if constexpr (IDLE) {
+      if constexpr (HANDOVER) store_stage(nbuf, st + 1, word_tag);
+      region_end();
+      if constexpr (RELOAD) {
+        if constexpr (D > 1) {
+          grp = grpn;
+          load_group(grpn, min((st + 2) / kGroup + 1, last / kGroup));
+        } else {
+          load_group(grp, (st + 2) / kGroup);
+        }
+      }
+      if constexpr (HANDOVER) load_stage(min(st + 1 + D, last), lmask, word_tag);
+      region_end();
+      __syncthreads();
+      return;
+    }
     WFrag w;
     AFrag a0, a1;
     Scales<C, RES> sc;
@@ -640,6 +668,7 @@ __device__ __forceinline__ void gemm_tile(
   if (st + 1 < nstages - 1) stage(st + 1, HO{}, W2{}, NoRl{});
   if (st + 2 < nstages - 1) stage(st + 2, HO{}, W3{}, NoRl{});
   stage(nstages - 1, NoHO{}, W0{}, NoRl{});
+  if constexpr (IDLE) return;
 
   if constexpr (SWIGLU) {
     swiglu_epilogue<C, HRES>(acc, so, M, m0 + wm * kTM + frow, n0 + wn * kTN, h);
