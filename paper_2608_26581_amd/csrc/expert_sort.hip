@@ -27,6 +27,7 @@ namespace {
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int64_t kOneGroup = 8192;           // pairs
 constexpr int64_t kMaxGroups = 64;
+constexpr int kHeld = 4;
 constexpr int kBatch = 16;                    // groups whose counts are loaded together
 
 int64_t pairs_per_group(int64_t P) {
@@ -93,7 +94,17 @@ __global__ __launch_bounds__(kThreads) void expert_place_kernel(
 
   for (int i = tid; i < kWaves * E; i += kThreads) next[i] = 0;
   __syncthreads();
-  for (int64_t p = mine.p0 + lane; p < mine.p1; p += 64) {
+  // The wave's first kHeld chunks of 64 pairs stay in registers.
+  int held[kHeld];
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const int64_t p = mine.p0 + 64 * i + lane;
+    held[i] = p < mine.p1 ? pairs.at(p) : E;
+  }
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i)
+    if (held[i] < E) atomicAdd(&next[wave * E + held[i]], 1);
+  for (int64_t p = mine.p0 + 64 * kHeld + lane; p < mine.p1; p += 64) {
     const int e = pairs.at(p);
     if (e < E) atomicAdd(&next[wave * E + e], 1);
   }
@@ -150,9 +161,7 @@ __global__ __launch_bounds__(kThreads) void expert_place_kernel(
   __syncthreads();
 
   const int bits = 32 - __builtin_clz(E);          // E itself stands for a dropped pair
-  for (int64_t c = mine.p0; c < mine.p1; c += 64) {
-    const int64_t p = c + lane;
-    const int e = p < mine.p1 ? pairs.at(p) : E;
+  auto place = [&](int64_t p, int e) {
     uint64_t same = ~0ull;
     for (int b = 0; b < bits; ++b) {
       const bool bit = (e >> b) & 1;
@@ -172,7 +181,12 @@ __global__ __launch_bounds__(kThreads) void expert_place_kernel(
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     if (p < mine.p1) slots[p] = slot;
-  }
+  };
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i)
+    if (mine.p0 + 64 * i < mine.p1) place(mine.p0 + 64 * i + lane, held[i]);
+  for (int64_t c = mine.p0 + 64 * kHeld; c < mine.p1; c += 64)
+    place(c + lane, c + lane < mine.p1 ? pairs.at(c + lane) : E);
   // Slots that no pair has.
   for (int64_t p = max((int64_t)total, g0) + tid; p < g1; p += kThreads) rows[p] = -1;
 }

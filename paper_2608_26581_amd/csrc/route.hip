@@ -7,11 +7,15 @@
 //     dl_i = sum_{j: S_j = i} dw_j w_j - s p_i / sum p.
 //
 // A row of logits lies in the registers of kLanes lanes, R consecutive ones a lane: 16
-// lanes (four rows a wave) up to 256 experts, the whole wave up to 1024.  A choice is a
-// scan of the lane's R, a maximum over the lanes and a minimum over the indices of those
-// that reach it (ties go to the lowest index), in DPP steps without LDS.  Logits are compared
-// as integers of the same order, with NaN above all, so that infinities and what was taken
-// (below -infinity, which is never chosen) need no case of their own.
+// lanes (four rows a wave) up to 256 experts, the whole wave up to 1024.  A choice is the
+// maximum of the lane's R and over the lanes, in DPP steps without LDS, then the lowest of the
+// indices that reach it.  Logits are compared as integers of the same order, with NaN above
+// all, so that infinities and what was taken (below -infinity, which is never chosen) need no
+// case of their own.  A bf16 logit leaves room for its index in the same integer, the lower the
+// larger: the maximum is then the choice itself.
+//
+// Bound by the instructions of the choices (5.5 R + 12 a choice for fp32, 2.5 R + 5 for bf16)
+// and, for a softmax over all logits, by their exponentials.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -22,17 +26,35 @@ namespace rfq {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTaken = INT32_MIN;              // below every logit's key
+constexpr int kTaken = INT32_MIN;              // below every key
 constexpr int kNever = (int)0x807FFFFF;        // the key of -infinity
 
 // Integers in the order of the floats: NaN above +infinity, -0 as +0.
-__device__ __forceinline__ int key_of(float v) {
+__device__ __forceinline__ int order_of(float v) {
   if (v != v) return INT32_MAX;
   const int b = __float_as_int(v + 0.0f);
   return b ^ ((b >> 31) & 0x7FFFFFFF);
 }
+// The key of logit `index`, and the value and (bf16) the index of a key.
+template <bool BF16>
+__device__ __forceinline__ int key_of(float v, int index) {
+  return BF16 ? (order_of(v) & (int)0xFFFF0000) | (0xFFFF ^ index) : order_of(v);
+}
+template <bool BF16>
 __device__ __forceinline__ float value_of(int key) {
-  return __int_as_float(key ^ ((key >> 31) & 0x7FFFFFFF));
+  const int b = key ^ ((key >> 31) & 0x7FFFFFFF);
+  return __int_as_float(BF16 ? b & (int)0xFFFF0000 : b);
+}
+__device__ __forceinline__ int index_of(int key) { return 0xFFFF ^ (key & 0xFFFF); }
+
+// exp(x) for x <= 0 (and NaN): 2^(x log2 e) with the product's rounding error, which grows with
+// |x|, multiplied back in.  Below -110, less than a float's least normal number, 0.
+__device__ __forceinline__ float exp_of(float x) {
+  x = x < -110.0f ? -110.0f : x;
+  constexpr float kHi = 1.44269502162933349609f, kLo = 1.92596303e-8f;   // log2(e)
+  const float h = x * kHi, l = fmaf(x, kHi, -h) + x * kLo;
+  const float e = __builtin_amdgcn_exp2f(h);
+  return fmaf(e * l, 0.693147182f, e);
 }
 
 // Combination of a lane's value with another's: all lanes of the row hold the result.
@@ -57,38 +79,44 @@ struct Max { __device__ int operator()(int a, int b) const { return max(a, b); }
 struct Min { __device__ int operator()(int a, int b) const { return min(a, b); } };
 struct Sum { __device__ float operator()(float a, float b) const { return a + b; } };
 
-// The lane's logits i0 .. i0 + R - 1 of a row (past E: kTaken) as keys.  VEC: E a multiple
+// Bytes of the loads that a lane's logits divide into.
+constexpr int piece_bytes(int bytes) {
+  return bytes % 16 == 0 ? 16 : (bytes % 8 == 0 ? 8 : (bytes % 4 == 0 ? 4 : 2));
+}
+
+// The lane's logits i0 .. i0 + R - 1 of a row (past E: -infinity) as keys.  VEC: E a multiple
 // of R and rows at multiples of the lane's bytes (at most 16).
 template <int R, bool BF16, bool VEC>
 __device__ __forceinline__ void load_keys(const void *row, int i0, int E, int (&key)[R]) {
   if constexpr (VEC) {
-    constexpr int kBytes = R * (BF16 ? 2 : 4), kPiece = kBytes < 16 ? kBytes : 16;
+    constexpr int kBytes = R * (BF16 ? 2 : 4), kPiece = piece_bytes(kBytes);
     constexpr int kPer = kPiece / (BF16 ? 2 : 4);
     if (i0 >= E) {
 #pragma unroll
-      for (int r = 0; r < R; ++r) key[r] = kTaken;
+      for (int r = 0; r < R; ++r) key[r] = key_of<BF16>(-INFINITY, i0 + r);
       return;
     }
     const uint8_t *p = static_cast<const uint8_t *>(row) + (int64_t)i0 * (BF16 ? 2 : 4);
 #pragma unroll
     for (int c = 0; c < kBytes / kPiece; ++c) {
       uint32_t w[4] = {0, 0, 0, 0};
+      const uint8_t *at = p + kPiece * c;
       if constexpr (kPiece == 16) {
-        const u32x4 v = *reinterpret_cast<const u32x4 *>(p + 16 * c);
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(at);
         w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
       } else if constexpr (kPiece == 8) {
-        const uint2 v = *reinterpret_cast<const uint2 *>(p);
+        const uint2 v = *reinterpret_cast<const uint2 *>(at);
         w[0] = v.x; w[1] = v.y;
       } else if constexpr (kPiece == 4) {
-        w[0] = *reinterpret_cast<const uint32_t *>(p);
+        w[0] = *reinterpret_cast<const uint32_t *>(at);
       } else {
-        w[0] = *reinterpret_cast<const uint16_t *>(p);
+        w[0] = *reinterpret_cast<const uint16_t *>(at);
       }
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
         const float f = BF16 ? __uint_as_float((i & 1) ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16)
                              : __uint_as_float(w[i]);
-        key[c * kPer + i] = key_of(f);
+        key[c * kPer + i] = key_of<BF16>(f, i0 + c * kPer + i);
       }
     }
   } else {
@@ -97,17 +125,17 @@ __device__ __forceinline__ void load_keys(const void *row, int i0, int E, int (&
       const int i = min(i0 + r, E - 1);
       const float f = BF16 ? __uint_as_float((uint32_t)static_cast<const uint16_t *>(row)[i] << 16)
                            : static_cast<const float *>(row)[i];
-      key[r] = i0 + r < E ? key_of(f) : kTaken;
+      key[r] = key_of<BF16>(i0 + r < E ? f : -INFINITY, i0 + r);
     }
   }
 }
 
-// sum of exp(l - m) over the row's logits (0 where all are -infinity; m is then unused).
-template <int kLanes, int R>
+// sum of exp(l - m) over the row's logits; m their largest (where that is -infinity, NaN).
+template <int kLanes, int R, bool BF16>
 __device__ __forceinline__ float exp_sum(const int (&key)[R], float m) {
   float s = 0.0f;
 #pragma unroll
-  for (int r = 0; r < R; ++r) s += key[r] > kNever ? expf(value_of(key[r]) - m) : 0.0f;
+  for (int r = 0; r < R; ++r) s += exp_of(value_of<BF16>(key[r]) - m);
   return over_row<kLanes>(s, Sum{});
 }
 
@@ -123,29 +151,38 @@ __global__ __launch_bounds__(kThreads) void route_kernel(const void *__restrict_
   int key[R];
   load_keys<R, BF16, VEC>(static_cast<const uint8_t *>(logits) + row * E * (BF16 ? 2 : 4), i0, E,
                           key);
-  int mine = kNever, mine_at = -1, top = kNever;
+  int left[R], mine = kNever, mine_at = -1, top = kNever;
   float total = 0.0f;
   for (int j = 0; j < k; ++j) {
-    int best = key[0], at = i0;
+    int best = key[0];
 #pragma unroll
-    for (int r = 1; r < R; ++r) {
-      at = key[r] > best ? i0 + r : at;
-      best = max(best, key[r]);
-    }
+    for (int r = 1; r < R; ++r) best = max(best, key[r]);
     const int most = over_row<kLanes>(best, Max{});
-    const int where = over_row<kLanes>(best == most ? at : INT32_MAX, Min{});
+    int where;
+    if constexpr (BF16) {
+      where = index_of(most);
+#pragma unroll
+      for (int r = 0; r < R; ++r) left[r] = key[r] == most ? kTaken : key[r];
+    } else {
+      int at = INT32_MAX;
+#pragma unroll
+      for (int r = R - 1; r >= 0; --r) at = key[r] == most ? i0 + r : at;
+      where = over_row<kLanes>(at, Min{});
+#pragma unroll
+      for (int r = 0; r < R; ++r) left[r] = where - i0 == r ? kTaken : key[r];
+    }
     if (j == 0) {
       top = most;
-      if (!renormalize) total = exp_sum<kLanes, R>(key, value_of(top));
+      if (!renormalize) total = exp_sum<kLanes, R, BF16>(key, value_of<BF16>(top));
     }
     if (lane == j) {
       mine = most;
       mine_at = most > kNever ? where : -1;
     }
 #pragma unroll
-    for (int r = 0; r < R; ++r) key[r] = i0 + r == where ? kTaken : key[r];
+    for (int r = 0; r < R; ++r) key[r] = left[r];
   }
-  const float e = mine > kNever ? expf(value_of(mine) - value_of(top)) : 0.0f;
+  const float e = mine > kNever ? exp_of(value_of<BF16>(mine) - value_of<BF16>(top)) : 0.0f;
   if (renormalize) total = over_row<kLanes>(e, Sum{});
   if (t < T && lane < k) {
     weights[t * k + lane] = mine_at >= 0 ? e / total : 0.0f;
@@ -180,11 +217,14 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(
     int best = key[0];
 #pragma unroll
     for (int r = 1; r < R; ++r) best = max(best, key[r]);
-    const float m = value_of(over_row<kLanes>(best, Max{}));
-    const float total = exp_sum<kLanes, R>(key, m);
+    const float top = value_of<BF16>(over_row<kLanes>(best, Max{}));
+    const bool none = top == -INFINITY;
+    const float m = none ? 0.0f : top;
+    const float sum = exp_sum<kLanes, R, BF16>(key, m);
+    const float per = none ? 0.0f : 1.0f / sum;
 #pragma unroll
     for (int r = 0; r < R; ++r)
-      d[r] = key[r] > kNever ? -(expf(value_of(key[r]) - m) / total) * s : 0.0f;
+      d[r] = -(exp_of(value_of<BF16>(key[r]) - m) * per) * s;
   }
   for (int j = 0; j < k; ++j) {
     const int i = __shfl(expert, j, kLanes);
@@ -196,23 +236,24 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(
   uint8_t *out = static_cast<uint8_t *>(dlogits) + (t * E + i0) * kElem;
   if constexpr (VEC) {
     if (i0 >= E) return;
-    uint32_t u[(R * kElem + 3) / 4];
+    constexpr int kBytes = R * kElem, kPiece = piece_bytes(kBytes);
+    uint32_t u[(kBytes + 3) / 4];
 #pragma unroll
-    for (int c = 0; c < (R * kElem + 3) / 4; ++c) {
-      if constexpr (BF16) u[c] = bf16x2_rne(d[2 * c], R > 1 ? d[(2 * c + 1) % R] : 0.0f);
+    for (int c = 0; c < (kBytes + 3) / 4; ++c) {
+      if constexpr (BF16) u[c] = bf16x2_rne(d[2 * c], 2 * c + 1 < R ? d[(2 * c + 1) % R] : 0.0f);
       else u[c] = __float_as_uint(d[c]);
     }
-    constexpr int kBytes = R * kElem;
-    if constexpr (kBytes >= 16) {
 #pragma unroll
-      for (int c = 0; c < kBytes / 16; ++c)
-        reinterpret_cast<u32x4 *>(out)[c] = u32x4{u[4 * c], u[4 * c + 1], u[4 * c + 2], u[4 * c + 3]};
-    } else if constexpr (kBytes == 8) {
-      *reinterpret_cast<uint2 *>(out) = make_uint2(u[0], u[1]);
-    } else if constexpr (kBytes == 4) {
-      *reinterpret_cast<uint32_t *>(out) = u[0];
-    } else {
-      *reinterpret_cast<uint16_t *>(out) = (uint16_t)u[0];
+    for (int c = 0; c < kBytes / kPiece; ++c) {
+      uint8_t *at = out + kPiece * c;
+      if constexpr (kPiece == 16)
+        *reinterpret_cast<u32x4 *>(at) = u32x4{u[4 * c], u[4 * c + 1], u[4 * c + 2], u[4 * c + 3]};
+      else if constexpr (kPiece == 8)
+        *reinterpret_cast<uint2 *>(at) = make_uint2(u[2 * c], u[2 * c + 1]);
+      else if constexpr (kPiece == 4)
+        *reinterpret_cast<uint32_t *>(at) = u[c];
+      else
+        *reinterpret_cast<uint16_t *>(at) = (uint16_t)(u[c / 2] >> (16 * (c & 1)));
     }
   } else {
 #pragma unroll
@@ -235,7 +276,10 @@ hipError_t on_shape(int E, Go go) {
   if (E <= 16) return go(Shape<16, 1>{});
   if (E <= 32) return go(Shape<16, 2>{});
   if (E <= 64) return go(Shape<16, 4>{});
+  if (E <= 96) return go(Shape<16, 6>{});
   if (E <= 128) return go(Shape<16, 8>{});
+  if (E <= 160) return go(Shape<16, 10>{});
+  if (E <= 192) return go(Shape<16, 12>{});
   if (E <= 256) return go(Shape<16, 16>{});
   if (E <= 512) return go(Shape<64, 8>{});
   return go(Shape<64, 16>{});
@@ -245,7 +289,7 @@ hipError_t on_shape(int E, Go go) {
 // inside a row.
 template <int R>
 bool vector_rows(const void *a, const void *b, int E, bool bf16) {
-  const int bytes = R * (bf16 ? 2 : 4), piece = bytes < 16 ? bytes : 16;
+  const int piece = piece_bytes(R * (bf16 ? 2 : 4));
   const uintptr_t p = reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b);
   return E % R == 0 && p % piece == 0;
 }

@@ -41,7 +41,7 @@ def check(l, k, renormalize):
 @pytest.mark.parametrize("renormalize", [True, False])
 @pytest.mark.parametrize("T,E,k", [
     (1, 1, 1), (3, 8, 2), (5, 16, 16), (1, 17, 4), (33, 31, 3), (17, 32, 8), (129, 60, 4),
-    (64, 64, 6), (7, 100, 1), (50, 128, 8), (21, 160, 6), (16, 255, 9), (9, 256, 8), (6, 257, 8),
+    (64, 64, 6), (7, 100, 1), (13, 90, 5), (11, 96, 6), (50, 128, 8), (21, 160, 6), (7, 157, 5), (8, 192, 8), (5, 186, 16), (16, 255, 9), (9, 256, 8), (6, 257, 8),
     (5, 511, 16), (5, 512, 2), (4, 1000, 10), (3, 1024, 16)])
 def test_choices_and_weights(T, E, k, renormalize, dtype):
     check(logits(T, E, dtype, T * E + k), k, renormalize)
