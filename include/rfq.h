@@ -698,14 +698,17 @@ rfq_status rfq_expert_sort(const int32_t *experts, int64_t T, int64_t k, int64_t
 int64_t rfq_expert_sort_workspace_bytes(int64_t T, int64_t k, int64_t E);
 
 /*
- * out[s] = x[rows[s]], a copy of the row; zeros where rows[s] is not in [0, T).
- *   x [T][N], out [P][N] of dtype, 16-byte aligned;  rows [P].
- * Rows take ceil(N / 512) of bf16 or ceil(N / 256) of fp32 (where N is not a multiple of 8,
- * or 4: ceil(N / 64)) units of work, which together stay below 2^26 - 4; the same holds for
- * the rows that rfq_expert_combine and its gradient go through (T).
+ * out[slots[t][j]] = x[t], copies of the rows, and zeros in the rows of out whose rows[s] is
+ * not in [0, T).  rows and slots belong together, as rfq_expert_sort writes them: a slot is
+ * named once.  Slots outside [0, P) are not written.
+ *   x [T][N], out [P][N] of dtype, 16-byte aligned;  rows [P];  slots [T][k].
+ * A row takes ceil(N / 512) of bf16 or ceil(N / 256) of fp32 (where N is not a multiple of 8,
+ * or 4: ceil(N / 64)) units of work; those of T rows and P / 16 together are at most
+ * 2^26 - 17, here and (without the P / 16) in rfq_expert_combine and its gradient.
  */
 rfq_status rfq_expert_gather(const void *x, rfq_dtype dtype, int64_t T, int64_t N,
-                             const int32_t *rows, int64_t P, void *out, void *hip_stream);
+                             const int32_t *rows, const int32_t *slots, int64_t k, int64_t P,
+                             void *out, void *hip_stream);
 
 /*
  * out[t] = sum_j weights[t][j] z[slots[t][j]] over the pairs whose slot is in [0, P); fp32

@@ -27,12 +27,16 @@ bool pairs_ok(int64_t T, int64_t k) {
 bool route_ok(int64_t T, int64_t E, int64_t k) {
   return pairs_ok(T, k) && E >= k && E <= rfq::kMaxExperts && T <= kMaxWorkItems / 64 - 4;
 }
-// Rows of N elements that waves copy in parts of 64 pieces (of 16 bytes, or of an element).
-bool rows_ok(int64_t rows, int64_t N, rfq_dtype dtype) {
-  if (rows < 0 || rows > INT32_MAX || N < 0 || N > INT32_MAX) return false;
+// Rows of N elements that waves go through in parts of 64 pieces (of 16 bytes, or of an
+// element), and with them workgroups of 256 for 64 of P slots.
+int64_t row_parts(int64_t rows, int64_t N, rfq_dtype dtype) {
   const int64_t bytes = N * size_of(dtype);
   const int64_t pieces = bytes % 16 == 0 ? bytes / 16 : N;
-  return rows * ((pieces + 63) / 64) <= kMaxWorkItems / 64 - 4;
+  return rows * ((pieces + 63) / 64);
+}
+bool rows_ok(int64_t rows, int64_t N, rfq_dtype dtype, int64_t P = 0) {
+  if (rows < 0 || rows > INT32_MAX || N < 0 || N > INT32_MAX) return false;
+  return row_parts(rows, N, dtype) + 4 * (P / 64) <= kMaxWorkItems / 64 - 16;
 }
 
 }  // namespace
@@ -94,15 +98,18 @@ rfq_status rfq_expert_sort(const int32_t *experts, int64_t T, int64_t k, int64_t
 }
 
 rfq_status rfq_expert_gather(const void *x, rfq_dtype dtype, int64_t T, int64_t N,
-                             const int32_t *rows, int64_t P, void *out, void *hip_stream) {
+                             const int32_t *rows, const int32_t *slots, int64_t k, int64_t P,
+                             void *out, void *hip_stream) {
   if (!valid_dtype(dtype)) return RFQ_ERR_DTYPE;
-  if (T < 0 || T > INT32_MAX || !rows_ok(P, N, dtype)) return RFQ_ERR_SHAPE;
+  if (P < 0 || P > INT32_MAX || !pairs_ok(T, k) || !rows_ok(T, N, dtype, P))
+    return RFQ_ERR_SHAPE;
   if (P == 0 || N == 0) return RFQ_OK;
-  if ((T > 0 && !x) || !rows || !out) return RFQ_ERR_NULL;
-  if (!aligned(x, 16) || !aligned(rows, 4) || !aligned(out, 16)) return RFQ_ERR_ALIGN;
+  if ((T > 0 && (!x || !slots)) || !rows || !out) return RFQ_ERR_NULL;
+  if (!aligned(x, 16) || !aligned(rows, 4) || !aligned(slots, 4) || !aligned(out, 16))
+    return RFQ_ERR_ALIGN;
   const rfq_status s = check_device();
   if (s != RFQ_OK) return s;
-  return launched(rfq::launch_expert_gather(x, dtype == RFQ_BF16, T, N, rows, P, out,
+  return launched(rfq::launch_expert_gather(x, dtype == RFQ_BF16, T, N, rows, slots, (int)k, P, out,
                                             stream_of(hip_stream)));
 }
 

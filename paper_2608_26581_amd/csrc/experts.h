@@ -28,7 +28,8 @@ hipError_t launch_expert_sort(const int32_t *experts, int64_t T, int k, int64_t 
                               int64_t workspace_bytes, hipStream_t stream);
 
 hipError_t launch_expert_gather(const void *x, bool bf16, int64_t T, int64_t N,
-                                const int32_t *rows, int64_t P, void *out, hipStream_t stream);
+                                const int32_t *rows, const int32_t *slots, int k, int64_t P,
+                                void *out, hipStream_t stream);
 // weights == nullptr: ones.
 hipError_t launch_expert_combine(const void *z, bool bf16, int64_t P, int64_t N,
                                  const int32_t *slots, const float *weights, int64_t T, int k,

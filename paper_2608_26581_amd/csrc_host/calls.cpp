@@ -12,6 +12,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/core/grad_mode.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -720,6 +721,12 @@ const at::Tensor *matrix(PyObject *o, int dev) {
   return t && float_code(*t) >= 0 ? t : nullptr;
 }
 
+// Whether autograd would have to see a call on these (its Python path does that).
+template <class... T>
+bool wants_grad(const T *...t) {
+  return at::GradMode::is_enabled() && ((t && t->requires_grad()) || ...);
+}
+
 // A plan's tensors: rows [T k] and slots [T][k] (the offsets have only to be ints).
 struct Plan { const at::Tensor *rows, *slots; int64_t T, k; };
 bool plan_of(PyObject *const *a, int dev, Plan &p) {
@@ -743,7 +750,7 @@ PyObject *route(PyObject *, PyObject *const *a, Py_ssize_t n) {
   const at::Tensor *l = matrix(a[0], dev);
   const int renormalize = PyObject_IsTrue(a[2]);
   if (renormalize < 0) return nullptr;
-  if (!l || k > l->size(1)) return none();
+  if (!l || k > l->size(1) || wants_grad(l)) return none();
   const int64_t T = l->size(0), E = l->size(1);
   at::Tensor t[2];
   parts(*l, {{{T, k}, at::kFloat}, {{T, k}, at::kInt}}, t);
@@ -831,9 +838,9 @@ PyObject *expert_gather(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (!x || x->size(0) != p.T) return none();
   const int64_t N = x->size(1), P = p.T * p.k;
   const at::Tensor y = rows_out(a[4], *x, P, N, dev);
-  if (!y.defined()) return none();
-  const int st = call(ex.expert_gather, x->data_ptr(), float_code(*x), p.T, N, int_data(p.rows), P,
-                      y.data_ptr(), stream_of(dev));
+  if (!y.defined() || wants_grad(x, &y)) return none();
+  const int st = call(ex.expert_gather, x->data_ptr(), float_code(*x), p.T, N, int_data(p.rows),
+                      int_data(p.slots), p.k, P, y.data_ptr(), stream_of(dev));
   return st ? failed(st) : result(a[4], y);
   END_HANDLE_TH_ERRORS
 }
@@ -857,7 +864,7 @@ PyObject *expert_combine(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (!z || z->size(0) != p.T * p.k) return none();
   const int64_t N = z->size(1);
   const at::Tensor y = rows_out(a[5], *z, p.T, N, dev);
-  if (!y.defined()) return none();
+  if (!y.defined() || wants_grad(z, w, &y)) return none();
   const int st = call(ex.expert_combine, z->data_ptr(), float_code(*z), p.T * p.k, N,
                       int_data(p.slots), float_data(w), p.T, p.k, y.data_ptr(), stream_of(dev));
   return st ? failed(st) : result(a[5], y);

@@ -101,7 +101,7 @@ def _dense(t):
 class _Route(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, k, renormalize):
-        weights, experts = _route(logits, k, renormalize, None)
+        weights, experts = rfq_route(logits, k, renormalize)
         ctx.mark_non_differentiable(experts)
         ctx.save_for_backward(logits, weights, experts)
         ctx.renormalize = renormalize
@@ -116,10 +116,6 @@ class _Route(torch.autograd.Function):
 
 
 def _route(logits, k, renormalize, stream):
-    if stream is None:
-        r = _native("route", logits, k, renormalize)
-        if r is not None:
-            return r
     _need_2d(logits, "logits", _FLOAT)
     dev, (T, E) = logits.get_device(), logits.shape
     k = int(k)
@@ -138,6 +134,10 @@ def rfq_route(logits, k, renormalize=True, stream=None):
     (weights [T][k] fp32, experts [T][k] int32): softmax over the chosen logits, or with
     renormalize False over all.  -inf is not chosen: expert -1, weight 0.  weights are
     differentiable in logits."""
+    if stream is None:
+        r = _native("route", logits, k, renormalize)
+        if r is not None:
+            return r
     if _wants_grad(logits):
         return _apply(_Route, stream, logits.device, logits, k, renormalize)
     return _route(logits, k, renormalize, stream)
@@ -207,7 +207,7 @@ class _Gather(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, offsets, rows, slots):
         ctx.save_for_backward(offsets, rows, slots)
-        return _gather(x, (offsets, rows, slots), None, None)
+        return rfq_expert_gather(x, (offsets, rows, slots))
 
     @staticmethod
     def backward(ctx, dxs):
@@ -215,10 +215,6 @@ class _Gather(torch.autograd.Function):
 
 
 def _gather(x, plan, out, stream):
-    if stream is None:
-        r = _native("expert_gather", x, *plan, out)
-        if r is not None:
-            return r if out is None else _written(out)
     _need_2d(x, "x", _FLOAT)
     dev, (T, N) = x.get_device(), x.shape
     rows, slots = _need_plan(plan, dev)
@@ -229,8 +225,8 @@ def _gather(x, plan, out, stream):
         out = _empty((P, N), x.dtype, x.device, stream)
     else:
         _need(out, "out", (x.dtype,), (P, N), dev)
-    st = load().rfq_expert_gather(_ptr(x), _dtype_code(x), T, N, _ptr(rows), P, _ptr(out),
-                                  _stream(stream, dev))
+    st = load().rfq_expert_gather(_ptr(x), _dtype_code(x), T, N, _ptr(rows), _ptr(slots),
+                                  slots.shape[1], P, _ptr(out), _stream(stream, dev))
     _check("rfq_expert_gather", st)
     return out if given is None else _written(out)
 
@@ -238,6 +234,10 @@ def _gather(x, plan, out, stream):
 def rfq_expert_gather(x, plan, out=None, stream=None):
     """xs [T k][N]: the rows of x [T][N] (bf16 or fp32) in the slots of the plan, zeros past the
     last.  Differentiable in x, without out."""
+    if stream is None:
+        r = _native("expert_gather", x, *plan, out)
+        if r is not None:
+            return r if out is None else _written(out)
     if _wants_grad(x, out):
         if out is not None:
             raise ValueError("out takes no gradient: x and out must not require one")
@@ -249,7 +249,7 @@ class _Combine(torch.autograd.Function):
     @staticmethod
     def forward(ctx, z, weights, offsets, rows, slots):
         ctx.save_for_backward(z, weights, offsets, rows, slots)
-        return _combine(z, weights, (offsets, rows, slots), None, None)
+        return rfq_expert_combine(z, weights, (offsets, rows, slots))
 
     @staticmethod
     @once_differentiable
@@ -266,7 +266,7 @@ class _Sum(torch.autograd.Function):
     @staticmethod
     def forward(ctx, z, offsets, rows, slots):
         ctx.save_for_backward(offsets, rows, slots)
-        return _combine(z, None, (offsets, rows, slots), None, None)
+        return rfq_expert_combine(z, None, (offsets, rows, slots))
 
     @staticmethod
     def backward(ctx, dout):
@@ -274,10 +274,6 @@ class _Sum(torch.autograd.Function):
 
 
 def _combine(z, weights, plan, out, stream):
-    if stream is None:
-        r = _native("expert_combine", z, weights, *plan, out)
-        if r is not None:
-            return r if out is None else _written(out)
     _need_2d(z, "z", _FLOAT)
     dev, (P, N) = z.get_device(), z.shape
     rows, slots = _need_plan(plan, dev)
@@ -301,6 +297,10 @@ def rfq_expert_combine(z, weights, plan, out=None, stream=None):
     """out [T][N]: the sum over a token's choices of its weight (fp32 [T][k]; None: 1) times
     the row of z [T k][N] (bf16 or fp32) in the choice's slot; dropped choices add nothing.
     Differentiable in z and weights, without out."""
+    if stream is None:
+        r = _native("expert_combine", z, weights, *plan, out)
+        if r is not None:
+            return r if out is None else _written(out)
     if _wants_grad(z, weights, out):
         if out is not None:
             raise ValueError("out takes no gradient: z, weights and out must not require one")

@@ -148,7 +148,7 @@ def _load():
     lib.rfq_expert_sort.argtypes = [P, I64, I64, I64, I64, P, P, P, P, I64, P]
     lib.rfq_expert_sort_workspace_bytes.argtypes = [I64] * 3
     lib.rfq_expert_sort_workspace_bytes.restype = I64
-    lib.rfq_expert_gather.argtypes = [P, I32, I64, I64, P, I64, P, P]
+    lib.rfq_expert_gather.argtypes = [P, I32, I64, I64, P, P, I64, I64, P, P]
     lib.rfq_expert_combine.argtypes = [P, I32, I64, I64, P, P, I64, I64, P, P]
     lib.rfq_expert_combine_backward.argtypes = [P, P, I32, I64, I64, P, P, P, I64, I64, P, P, P]
     lib.rfq_gemm_experts.argtypes = [P] * 8 + [I64] * 5 + [P, I32, P]

@@ -77,8 +77,8 @@ def test_combine_and_gradient(shape, dtype):
 
 def test_slots_and_rows_that_are_none():
     x, z = randn((4, 40), "bf16", 1), randn((8, 40), "bf16", 2)
-    rows = torch.tensor([0, 4, -1, 2 ** 31 - 1, 3, 3, -2 ** 31, 1], dtype=torch.int32).cuda()
-    slots = torch.tensor([[0, 8], [-1, 7], [2 ** 31 - 1, -2 ** 31], [4, 4]], dtype=torch.int32).cuda()
+    rows = torch.tensor([0, 4, 3, 2 ** 31 - 1, 3, -1, -2 ** 31, 1], dtype=torch.int32).cuda()
+    slots = torch.tensor([[0, 8], [-1, 7], [2 ** 31 - 1, -2 ** 31], [4, 2]], dtype=torch.int32).cuda()
     plan = (torch.tensor([0, 8], dtype=torch.int32).cuda(), rows, slots)
     got = rfq.rfq_expert_gather(x, plan)
     ok = (rows >= 0) & (rows < 4)
@@ -88,7 +88,12 @@ def test_slots_and_rows_that_are_none():
     assert ((got - want).abs() <= 2.0 ** -8 * want.abs()).all()
     dz, dw = rfq.rfq_expert_combine_backward(x, z, None, plan)
     assert (dw[2] == 0).all() and dw[0, 1] == 0 and dw[1, 0] == 0
-    assert (dz[~ok] == 0).all() and torch.equal(dz[0], x[0]) and torch.equal(dz[7], x[1])
+    assert torch.equal(dz, rfq.rfq_expert_gather(x, plan))
+    # A slot that two choices name is read twice.
+    slots[3, 1] = 4
+    got = rfq.rfq_expert_combine(z, None, plan).double().cpu()
+    want = taken(z, slots).sum(1)
+    assert ((got - want).abs() <= 2.0 ** -8 * want.abs()).all()
 
 
 def test_masked_places_have_no_influence():

@@ -59,13 +59,14 @@ def test_sort():
 
 
 def test_gather():
-    call = _caller("rfq_expert_gather", dict(x=A, dt=1, T=4, N=64, r=A, P=0, o=A, s=None))
-    assert call() == OK and call(N=0, P=3, x=None, r=None, o=None) == OK
+    call = _caller("rfq_expert_gather", dict(x=A, dt=1, T=4, N=64, r=A, sl=A, k=2, P=0, o=A, s=None))
+    assert call() == OK and call(N=0, P=3, x=None, r=None, sl=None, o=None) == OK
     _all(call, EDTYPE, dict(dt=2))
     _all(call, ESHAPE, dict(T=-1), dict(P=-1), dict(N=-1), dict(T=1 << 31), dict(P=1 << 31),
-         dict(N=1 << 31), dict(P=1 << 26), dict(P=1 << 20, N=1 << 20))
-    _all(call, ENULL, dict(P=3, x=None), dict(P=3, r=None), dict(P=3, o=None))
-    _all(call, EALIGN, dict(P=3, x=MIS), dict(P=3, r=A + 2), dict(P=3, o=MIS))
+         dict(N=1 << 31), dict(T=1 << 26), dict(T=1 << 20, N=1 << 20), dict(P=(1 << 30) + 64),
+         dict(k=0), dict(k=17))
+    _all(call, ENULL, dict(P=3, x=None), dict(P=3, r=None), dict(P=3, sl=None), dict(P=3, o=None))
+    _all(call, EALIGN, dict(P=3, x=MIS), dict(P=3, r=A + 2), dict(P=3, sl=A + 1), dict(P=3, o=MIS))
 
 
 def test_combine():
@@ -111,7 +112,7 @@ def test_product():
 @pytest.mark.parametrize("func,args", [
     ("rfq_route", (A, 1, 4, 64, 8, 1, A, A, None)),
     ("rfq_expert_sort", (A, 4, 2, 0, 8, A, A, A, None, 0, None)),
-    ("rfq_expert_gather", (A, 1, 4, 64, A, 3, A, None)),
+    ("rfq_expert_gather", (A, 1, 4, 64, A, A, 2, 3, A, None)),
     ("rfq_gemm_experts", (A, A, A, A, A, A, A, A, 4, 4, 2, 64, 64, A, 1, None)),
 ])
 def test_a_call_without_a_device_is_refused(func, args):
