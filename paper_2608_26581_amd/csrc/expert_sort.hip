@@ -19,6 +19,7 @@
 #include <atomic>
 
 #include "experts.h"
+#include "experts_device.h"
 #include "rfq_internal.h"
 
 namespace rfq {
@@ -46,16 +47,6 @@ struct Pairs {
     return e >= 0 && e < E ? (int)e : E;
   }
 };
-
-__device__ __forceinline__ int wave_inclusive(int v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int o = __shfl_up(v, d);
-    if (lane >= d) v += o;
-  }
-  return v;
-}
 
 // The pairs [p0, p1) that this wave places; p0 a multiple of 64 from the group's start.
 struct Range { int64_t p0, p1; };
@@ -139,7 +130,7 @@ __global__ __launch_bounds__(kThreads) void expert_place_kernel(
   } else if (tid < E) {
     for (int w = 0; w < kWaves; ++w) all += next[w * E + tid];
   }
-  const int incl = wave_inclusive(all);
+  const int incl = wave_inclusive_sum(all);
   if (lane == 63) part[wave] = incl;
   __syncthreads();
   int base = 0, total = 0;
@@ -151,10 +142,13 @@ __global__ __launch_bounds__(kThreads) void expert_place_kernel(
     const int first = base + incl - all;
     if (blockIdx.x == 0) offsets[tid] = first;
     int at = first + before;
+    int c[kWaves];           // (Read before the first is written: one round trip.)
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) c[w] = next[w * E + tid];
+#pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const int c = next[w * E + tid];
       next[w * E + tid] = at;
-      at += c;
+      at += c[w];
     }
   }
   if (tid == 0 && blockIdx.x == 0) offsets[E] = total;
