@@ -186,11 +186,8 @@ __global__ __launch_bounds__(kFewThreads) void rfq_gemm_experts_few_kernel(Exper
 // ---- many rows
 
 template <class C, bool RES, bool ZBF16, bool GK>
-__device__ __forceinline__ void many_tile(const ExpertsGemm &a, const ExpertTiles &ex) {
-  RowTile tile;
-  if (!expert_tile<C::kBM, 1024 / C::kBM, true>(ex, (int)blockIdx.x,
-                                                (int)((a.N + C::kBN - 1) / C::kBN), tile))
-    return;
+__device__ __forceinline__ void multiply_tile(const ExpertsGemm &a, const ExpertTiles &ex,
+                                              const RowTile &tile) {
   auto go = [&](auto idle) {
     gemm_tile<C, RES, ZBF16, false, false, false, false, GK, true, decltype(idle)::value>(
         a.qc, a.qs, a.rc, a.rs, a.wc, a.ws, a.M, a.N, a.K, a.z, SwigluOut{}, nullptr, a.K, ex, tile);
@@ -201,10 +198,25 @@ __device__ __forceinline__ void many_tile(const ExpertsGemm &a, const ExpertTile
     go(std::true_type{});
 }
 
+// A tile of C; with S another shape of the same columns, that one where it holds the rest of
+// the expert.
+template <class C, class S, bool RES, bool ZBF16, bool GK>
+__device__ __forceinline__ void many_tile(const ExpertsGemm &a, const ExpertTiles &ex) {
+  static_assert(C::kBN == S::kBN && C::kThreads == S::kThreads, "the same columns and waves");
+  RowTile tile;
+  if (!expert_tile<C::kBM, 1024 / C::kBM, true>(ex, (int)blockIdx.x,
+                                                (int)((a.N + C::kBN - 1) / C::kBN), tile))
+    return;
+  if constexpr (!std::is_same<C, S>::value) {
+    if (tile.end - tile.s0 <= S::kBM) return multiply_tile<S, RES, ZBF16, GK>(a, ex, tile);
+  }
+  multiply_tile<C, RES, ZBF16, GK>(a, ex, tile);
+}
+
 template <bool RES, bool ZBF16, bool GK>
 __global__ __launch_bounds__(Big::kThreads, 2) void rfq_gemm_experts_many_kernel(ExpertsGemm a,
                                                                                  ExpertTiles ex) {
-  many_tile<Big, RES, ZBF16, GK>(a, ex);
+  many_tile<Big, Half, RES, ZBF16, GK>(a, ex);
 }
 
 // The first `tiles` workgroups take the experts with many slots, the others those with few,
@@ -215,7 +227,7 @@ __global__ __launch_bounds__(Mid::kThreads, 3) void rfq_gemm_experts_both_kernel
     ExpertsGemm a, ExpertTiles many, ExpertTiles few, int tiles) {
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
   if ((int)blockIdx.x < tiles)
-    many_tile<Mid, RES, ZBF16, GK>(a, many);
+    many_tile<Mid, Mid, RES, ZBF16, GK>(a, many);
   else
     few_tile<RES, ZBF16, 2>(a, few, (int)blockIdx.x - tiles,
                             reinterpret_cast<v4f(*)[kFrags][64]>(smem));

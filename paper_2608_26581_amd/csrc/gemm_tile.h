@@ -41,6 +41,9 @@ using MidDeep = Tile<2, 2, 2, 2>;
 // 256 x 128, 8 waves of 64 x 64, one workgroup per CU: for grids of one to two
 // 128 x 128 tiles per CU, where half of the CUs would run two and half one.
 using Tall = Tile<4, 2, 2, 2>;
+// 128 x 256, 8 waves of 64 x 64: the lower half of a 256 x 256 tile of an expert that ends in
+// its upper one.
+using Half = Tile<2, 4, 2, 1>;
 
 constexpr int kStageK = 128;
 constexpr int kRowBytes = kStageK / 2;
@@ -524,7 +527,7 @@ __device__ __forceinline__ void gemm_tile(
   auto res_mask = [&](int st) -> int {
     const uint32_t w = phi_word(st);
     constexpr int kStep = kRPL / kPhiRows;
-    static_assert(kBM / kRPL == 2, "two residual row blocks per thread");
+    static_assert(!PHI || kBM / kRPL == 2, "two residual row blocks per thread");
     return (((w >> (8 * lw)) & 0xFFu) ? 1 : 0) | (((w >> (8 * (lw + kStep))) & 0xFFu) ? 2 : 0);
   };
   // ---- prologue: stage 0 into buffer 0, stage 1 in registers.
