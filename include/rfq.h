@@ -742,7 +742,8 @@ rfq_status rfq_expert_combine_backward(const void *dout, const void *z, rfq_dtyp
  * a row of zeros.  Rows of z that belong to no expert are not written.  Accumulation is fp32
  * in an unspecified order that does not change from call to call; codes whose products
  * overflow or whose scale byte is 0xFF reach only their own row or column of the result.
- *   q_codes [M][K/2], q_scales [M][K/32];  r_codes, r_scales the residual's, or both NULL.
+ *   q_codes [M][K/2], q_scales [M][K/32], M > 0 where there are slots;  r_codes, r_scales the
+ *           residual's, or both NULL.
  *   w_codes [E][N][K/2], w_scales [E][N][K/32]: rfq_quantize_weight of [E * N][K].
  *   offsets [E + 1], not decreasing and cut to [0, P];  rows [P] or NULL (then P == M).
  *   z       [P][N] row-major, z_dtype.

@@ -164,8 +164,8 @@ rfq_status rfq_gemm_experts(const uint8_t *q_codes, const uint8_t *q_scales,
       M * (K / 2) >= most || N * (K / 2) >= most || !rfq::gemm_experts_fits(P, E, N))
     return RFQ_ERR_SHAPE;
   if (P == 0 || N == 0 || E == 0) return RFQ_OK;
-  if ((M > 0 && (!q_codes || !q_scales)) || !w_codes || !w_scales || !offsets || !z)
-    return RFQ_ERR_NULL;
+  if (M == 0) return RFQ_ERR_SHAPE;
+  if (!q_codes || !q_scales || !w_codes || !w_scales || !offsets || !z) return RFQ_ERR_NULL;
   if ((r_codes == nullptr) != (r_scales == nullptr)) return RFQ_ERR_NULL;
   for (const void *p : {(const void *)q_codes, (const void *)q_scales, (const void *)r_codes,
                         (const void *)r_scales, (const void *)w_codes, (const void *)w_scales,

@@ -45,7 +45,7 @@ struct ExpertsGemm {
   const uint8_t *wc, *ws;             // weights [E][N]
   const int32_t *offsets;             // [E + 1]
   const int32_t *rows;                // [P], or nullptr: row p is slot p's
-  int64_t M, P, N, K;
+  int64_t M, P, N, K;                 // M > 0
   int E;
   void *z;                            // [P][N]
 };

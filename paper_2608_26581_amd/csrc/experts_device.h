@@ -69,7 +69,9 @@ struct TileCount {
   }
   // The expert of row tile t (below total), its slots and its first row tile; -1 if none.
   __device__ __forceinline__ int find(const ExpertTiles &x, int t, Slots &s, int &first) const {
-    const int l = __builtin_ctzll(__ballot(incl > t));
+    const uint64_t past = __ballot(incl > t);
+    if (!past) return -1;
+    const int l = __builtin_ctzll(past);
     first = __builtin_amdgcn_readlane(incl - mine, l);
     int e = l * per;
     if (per <= kHeld) {
@@ -110,12 +112,14 @@ __device__ __forceinline__ bool expert_tile(const ExpertTiles &x, int bid, int n
   int first;
   if ((tile.e = count.find(x, t / ntn, s, first)) < 0) return false;
   const int at = t - first * ntn, ntm = TileCount<kRows>::tiles(s);
-  const int group = at / (GM * ntn), size = min(ntm - group * GM, GM);
+  const int group = at / (GM * ntn), size = max(min(ntm - group * GM, GM), 1);
   const int in = at - group * GM * ntn;
   tile.s0 = s.begin + (group * GM + in % size) * kRows;
   tile.end = s.end;
   tile.tn = in / size;
-  return true;
+  // (With decreasing offsets the counts can pass 32 bits: nothing is read or written outside
+  // then either.)
+  return tile.s0 >= s.begin && tile.s0 < s.end && tile.tn >= 0 && tile.tn < ntn;
 }
 
 // The activation row of a slot, as an unsigned number: an index outside the activations is

@@ -60,18 +60,15 @@ __device__ __forceinline__ void few_tile(const ExpertsGemm &a, const ExpertTiles
   const int kblocks = (int)(a.K / 32), steps = (kblocks + 3) / 4;
   const int s0 = steps * wave / kFewWaves, s1 = steps * (wave + 1) / kFewWaves;
   RowTile tile;
-  if (!expert_tile<kFewRows, 1 << 20, false>(ex, bid, (int)((a.N + kFewCols - 1) / kFewCols), tile))
+  if (!expert_tile<kFewRows, 64, false>(ex, bid, (int)((a.N + kFewCols - 1) / kFewCols), tile))
     return;
   const int n0 = tile.tn * kFewCols;
   auto rsrc = [](const void *p, int64_t bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), (short)0, (int)bytes, 0x00020000);
   };
-  // (Never empty, so that a range exceeds every scalar offset: without activations the
-  // launch passes weights, and no lane's row is live.)
-  const int64_t held = max(a.M, (int64_t)1);
-  const __amdgpu_buffer_rsrc_t rq = rsrc(a.qc, held * kbytes), rqs = rsrc(a.qs, held * kblocks),
-                               rr = rsrc(RES ? a.rc : a.qc, held * kbytes),
-                               rrs = rsrc(RES ? a.rs : a.qs, held * kblocks),
+  const __amdgpu_buffer_rsrc_t rq = rsrc(a.qc, a.M * kbytes), rqs = rsrc(a.qs, a.M * kblocks),
+                               rr = rsrc(RES ? a.rc : a.qc, a.M * kbytes),
+                               rrs = rsrc(RES ? a.rs : a.qs, a.M * kblocks),
                                rw = rsrc(a.wc + (int64_t)tile.e * a.N * kbytes, a.N * kbytes),
                                rws = rsrc(a.ws + (int64_t)tile.e * a.N * kblocks, a.N * kblocks);
   // Step s + u of an operand; steps past the wave's last, and blocks past K, load zeros.
@@ -289,7 +286,7 @@ hipError_t launch_many(const ExpertsGemm &g, const ExpertTiles &ex, hipStream_t 
 // Few-row tiles alone up to four slots an expert (128 experts of 2048 x 768, 64 tokens: few
 // 23.5 us, both 26.5, at 128 tokens 33.9 and 32.5; 8 experts of 4096 x 4096, 16 tokens 21.4 and
 // 26.3), as long as a single expert that has all of them costs little.
-bool use_few(const ExpertsGemm &g) { return g.M == 0 || (g.P <= 4 * (int64_t)g.E && g.P <= 1024); }
+bool use_few(const ExpertsGemm &g) { return g.P <= 4 * (int64_t)g.E && g.P <= 1024; }
 // 256 x 256 tiles from 96 slots an expert where 128 x 128 ones would number two a CU (8 experts
 // of 4096 x 4096: 256 slots each 51.6 us, both 62; 128 each, 384 tiles, 46 and 38).
 bool use_many(const ExpertsGemm &g) {
@@ -309,9 +306,7 @@ bool gemm_experts_fits(int64_t P, int64_t E, int64_t N) {
   return (P / 128 + 2 * E) == 0 || (N + 63) / 64 <= ((1 << 24) - 16) / (P / 128 + 2 * E);
 }
 
-hipError_t launch_gemm_experts(const ExpertsGemm &args, bool z_bf16, hipStream_t stream) {
-  ExpertsGemm g = args;
-  if (g.M == 0) g.qc = g.wc, g.qs = g.ws, g.rc = nullptr, g.rs = nullptr;
+hipError_t launch_gemm_experts(const ExpertsGemm &g, bool z_bf16, hipStream_t stream) {
   const ExpertTiles ex{g.offsets, g.rows, g.E, (int)g.P, 0, INT32_MAX};
   const bool short_k = g.K <= kShortK, gk = g.K % (kStageK * kGroup) != 0;
   auto go = [&](auto res, auto zb) {

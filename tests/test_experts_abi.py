@@ -100,8 +100,9 @@ def test_product():
     assert call() == OK and call(**none) == OK
     assert call(P=4, N=0, **none) == OK and call(P=4, E=0, **none) == OK
     assert call(rows=None, M=0, **none) == OK
+    assert call(M=0) == OK and call(M=0, P=4, E=0) == OK
     _all(call, EDTYPE, dict(dt=2))
-    _all(call, ESHAPE, dict(M=-1), dict(P=-1), dict(E=-1), dict(N=-1), dict(K=0), dict(K=48),
+    _all(call, ESHAPE, dict(M=0, P=4), dict(M=-1), dict(P=-1), dict(E=-1), dict(N=-1), dict(K=0), dict(K=48),
          dict(E=1025), dict(rows=None, P=3), dict(M=1 << 31), dict(P=1 << 31), dict(N=1 << 31),
          dict(M=1 << 27), dict(N=1 << 27), dict(P=1 << 30, N=1 << 20), dict(K=1 << 32))
     _all(call, ENULL, *(dict(P=4, **{n: None}) for n in ("qc", "qs", "rc", "rs", "wc", "ws", "off", "z")))

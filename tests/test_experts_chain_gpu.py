@@ -73,3 +73,36 @@ def test_layer_captured_with_new_inputs():
         want = layer(x, logits, 2, w, 0)[-1]
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+def test_padded_tokens_and_masked_experts():
+    """A padded token's row holds anything and its logits -infinity: its result is zeros, and
+    nothing else changes.  A masked expert gets no token."""
+    x, logits, w = make(50, 8, 256, 96, 8, 7)
+    logits[:, 3] = -float("inf")
+    _, first, plan1, q1, g1, *_ = layer(x, logits, 2, w, 0)
+    pad = torch.tensor([0, 17, 49], device="cuda")
+    x2, logits2 = x.clone(), logits.clone()
+    x2[pad] = 3e38
+    logits2[pad] = -float("inf")
+    weights, experts, plan, _, g2, *_, out = layer(x2, logits2, 2, w, 0)
+    assert (experts[pad] == -1).all() and (weights[pad] == 0).all() and (plan.slots[pad] == -1).all()
+    assert (out[pad] == 0).all()
+    keep = torch.ones(50, dtype=torch.bool, device="cuda")
+    keep[pad] = False
+    assert torch.equal(experts[keep], first[keep])
+    # The slots move, and with them the order of the sums: either run's gate product is within
+    # its sums' rounding and half a step of bf16 of the same value.
+    s1, s2 = plan1.slots[keep].flatten().long(), plan.slots[keep].flatten().long()
+    v, bound, _ = ref.product(q1, w["gate"], plan1.offsets, plan1.rows, 50)
+    tol = 2 * (TOL_SUM * bound + 2.0 ** -8 * v.abs())
+    assert ((g1[s1] - g2[s2]).abs().double().cpu() <= tol[s1.cpu()]).all()
+    ends = plan.offsets.tolist()
+    assert ends[3] == ends[4] and ends[8] == 94
+
+
+def test_layer_of_one_token_and_one_expert():
+    x, logits, w = make(1, 1, 64, 32, 1, 8)
+    weights, experts, plan, q, g, u, h, z, out = layer(x, logits, 1, w, 0)
+    assert weights.item() == 1.0 and experts.item() == 0 and plan.offsets.tolist() == [0, 1]
+    assert torch.equal(out, z)

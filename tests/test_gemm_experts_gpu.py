@@ -179,8 +179,8 @@ def test_empty_and_refusals():
     none = [t[:0] if t is not None else None for t in a]
     assert rfq.rfq_gemm_experts(*none, *w, ints([0, 0, 0])).shape == (0, 32)
     assert rfq.rfq_gemm_experts(*a, w[0][:, :0].contiguous(), w[1][:, :0].contiguous(), off).shape == (8, 0)
-    z = rfq.rfq_gemm_experts(*none, *w, off, rows=ints([0] * 8))     # no activations: zeros
-    assert (z == 0).all()
+    with pytest.raises(rfq.RfqError, match="RFQ_ERR_SHAPE"):        # slots without activations
+        rfq.rfq_gemm_experts(*none, *w, off, rows=ints([0] * 8))
     with pytest.raises(ValueError, match="3-D"):
         rfq.rfq_gemm_experts(*a, w[0][0], w[1][0], off)
     with pytest.raises(ValueError, match="offsets"):
