@@ -46,7 +46,8 @@ LENGTHS = [
     ([1], 16, 32), ([3, 0, 1], 17, 64), ([0, 0, 5, 0], 33, 96), ([16, 17, 1, 15], 64, 128),
     ([0, 40, 0, 0, 25], 100, 160), ([2] * 9, 1, 512), ([1] * 70, 48, 544), ([64, 65, 63], 130, 1024),
     ([7, 129, 128, 1, 0, 200], 256, 512), ([300, 5], 200, 320), ([0, 513, 257], 260, 768),
-    ([33] * 5, 96, 4128), ([9, 8, 17, 16, 1, 30], 72, 2048), ([40] * 40, 100, 96),
+    ([33] * 5, 96, 4128), ([3, 0, 2, 5], 33, 128), ([5, 20, 0, 3], 70, 4608), ([2, 30], 33, 4224),
+    ([3, 1], 40, 8320), ([4, 16, 1], 65, 4096), ([9, 8, 17, 16, 1, 30], 72, 2048), ([40] * 40, 100, 96),
     # Enough tiles for the largest ones.
     ([700, 400], 8200, 96), ([0, 1000, 129, 1], 9000, 512),
 ]
