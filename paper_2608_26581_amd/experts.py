@@ -4,7 +4,9 @@ sorted by expert and back, and the product with a weight matrix per expert.
 Each function carries the name of the C entry point it calls and checks its
 tensors as the other calls do.  A plan is an ExpertPlan, or any three tensors of its
 layout.  The router's weights are differentiable in the logits, gather in x and
-combine in z and the weights; what goes through the 4-bit product is not.
+combine in z and the weights; what goes through the 4-bit product is not.  A backward
+pass is captured into a graph as torch has it for any: after a pass on a side stream, and
+with no eager graph of the same leaves left alive.
 """
 import ctypes
 import threading
