@@ -654,6 +654,7 @@ int64_t rfq_kv_attention_workspace_bytes(int64_t T, int64_t Hq, int64_t heads, i
  *   offsets [E + 1]  the slots of expert e are offsets[e] .. offsets[e + 1] - 1.
  *   rows    [P]      the token of each slot, -1 past the last.
  *   slots   [T][k]   the slot of each pair, -1 for a dropped one.
+ * Outputs overlap neither each other nor the inputs.
  */
 
 /*
@@ -704,7 +705,8 @@ int64_t rfq_expert_sort_workspace_bytes(int64_t T, int64_t k, int64_t E);
  *   x [T][N], out [P][N] of dtype, 16-byte aligned;  rows [P];  slots [T][k].
  * A row takes ceil(N / 512) of bf16 or ceil(N / 256) of fp32 (where N is not a multiple of 8,
  * or 4: ceil(N / 64)) units of work; those of T rows and P / 16 together are at most
- * 2^26 - 17, here and (without the P / 16) in rfq_expert_combine and its gradient.
+ * 2^26 - 17, here and (without the P / 16) in rfq_expert_combine and its gradient, and N + 256
+ * is below 2^31.
  */
 rfq_status rfq_expert_gather(const void *x, rfq_dtype dtype, int64_t T, int64_t N,
                              const int32_t *rows, const int32_t *slots, int64_t k, int64_t P,

@@ -35,7 +35,8 @@ int64_t row_parts(int64_t rows, int64_t N, rfq_dtype dtype) {
   return rows * ((pieces + 63) / 64);
 }
 bool rows_ok(int64_t rows, int64_t N, rfq_dtype dtype, int64_t P = 0) {
-  if (rows < 0 || rows > INT32_MAX || N < 0 || N > INT32_MAX) return false;
+  // (A lane's piece numbers go up to 256 past the row's last, in 32 bits.)
+  if (rows < 0 || rows > INT32_MAX || N < 0 || N >= INT32_MAX - 255) return false;
   return row_parts(rows, N, dtype) + 4 * (P / 64) <= kMaxWorkItems / 64 - 16;
 }
 

@@ -92,6 +92,19 @@ def test_combine_backward():
          dict(dz=MIS), dict(dw=A + 2))
 
 
+@pytest.mark.parametrize("func", ["gather", "combine", "combine_backward"])
+def test_rows_whose_pieces_pass_32_bits(func):
+    args = {"gather": dict(x=A, dt=1, T=0, N=64, r=A, sl=A, k=2, P=0, o=A, s=None),
+            "combine": dict(z=A, dt=1, P=8, N=64, sl=A, w=A, T=0, k=2, o=A, s=None),
+            "combine_backward": dict(d=A, z=A, dt=1, P=0, N=64, r=A, sl=A, w=A, T=0, k=2, dz=A,
+                                     dw=A, s=None)}[func]
+    call = _caller("rfq_expert_" + func, args)
+    most = (1 << 31) - 257                   # N + 256 below 2^31
+    assert call(N=most) == OK and call(N=most, dt=0) == OK
+    _all(call, ESHAPE, *(dict(N=n, dt=dt) for dt in (0, 1)
+                         for n in (most + 1, most + 2, (1 << 31) - 8, (1 << 31) - 1)))
+
+
 def test_product():
     call = _caller("rfq_gemm_experts",
                    dict(qc=A, qs=A, rc=A, rs=A, wc=A, ws=A, off=A, rows=A, M=4, P=0, E=2, N=64, K=64,
