@@ -172,7 +172,7 @@ __global__ __launch_bounds__(kThreads) void expert_place_kernel(
       if ((same >> lane) == 1) next[wave * E + e] = slot + 1;
       rows[slot] = (int)((uint32_t)p / (uint32_t)k);
     }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
     if (p < mine.p1) slots[p] = slot;
   };
