@@ -13,6 +13,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/core/grad_mode.h>
+#include <c10/core/AutogradState.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -721,10 +722,13 @@ const at::Tensor *matrix(PyObject *o, int dev) {
   return t && float_code(*t) >= 0 ? t : nullptr;
 }
 
-// Whether autograd would have to see a call on these (its Python path does that).
+// Whether autograd would have to see a call on these (its Python path does that): one
+// requires a gradient, or has a tangent of the forward mode (torch has one level of it).
 template <class... T>
 bool wants_grad(const T *...t) {
-  return at::GradMode::is_enabled() && ((t && t->requires_grad()) || ...);
+  return (at::GradMode::is_enabled() && ((t && t->requires_grad()) || ...)) ||
+         (c10::AutogradState::get_tls_state().get_fw_grad_mode() &&
+          ((t && t->_fw_grad(0).defined()) || ...));
 }
 
 // A plan's tensors: rows [T k] and slots [T][k] (the offsets have only to be ints).

@@ -4,15 +4,17 @@ sorted by expert and back, and the product with a weight matrix per expert.
 Each function carries the name of the C entry point it calls and checks its
 tensors as the other calls do.  A plan is an ExpertPlan, or any three tensors of its
 layout.  The router's weights are differentiable in the logits, gather in x and
-combine in z and the weights; what goes through the 4-bit product is not.  A backward
-pass is captured into a graph as torch has it for any: after a pass on a side stream, and
-with no eager graph of the same leaves left alive.
+combine in z and the weights, in reverse mode (a tangent of the forward mode is an
+error); what goes through the 4-bit product is not.  A backward pass is captured into a
+graph as torch has it for any: after a pass on a side stream, and with no eager graph of the
+same leaves left alive.
 """
 import ctypes
 import threading
 from typing import NamedTuple
 
 import torch
+from torch.autograd.forward_ad import unpack_dual
 from torch.autograd.function import once_differentiable
 
 from . import rfq as _binding
@@ -76,8 +78,12 @@ def _need_plan(plan, dev):
 
 
 def _wants_grad(*tensors):
-    return torch.is_grad_enabled() and any(
-        isinstance(t, torch.Tensor) and t.requires_grad for t in tensors)
+    """Whether autograd has to see a call on these: one requires a gradient, or has a tangent
+    of the forward mode, which the functions below do not have and torch then refuses."""
+    reverse = torch.is_grad_enabled()
+    return any(isinstance(t, torch.Tensor)
+               and (reverse and t.requires_grad or unpack_dual(t).tangent is not None)
+               for t in tensors)
 
 
 def _apply(function, stream, device, *args):

@@ -1,0 +1,68 @@
+"""Forward-mode differentiation of route, gather and combine: they have reverse mode only, and
+a tangent that comes in is refused as torch refuses it for such functions, on the native calls
+and on the binding's Python path (which an explicit stream takes), never dropped."""
+import pytest
+import torch
+import torch.autograd.forward_ad as forward_ad
+
+import paper_2608_26581_amd as rfq
+
+pytestmark = pytest.mark.gpu
+
+T, E, k, N = 12, 8, 3, 32
+
+
+def inputs():
+    g = torch.Generator(device="cuda").manual_seed(1)
+    l = torch.randn((T, E), generator=g, device="cuda")
+    x = torch.randn((T, N), generator=g, device="cuda").bfloat16()
+    z = torch.randn((T * k, N), generator=g, device="cuda").bfloat16()
+    w, experts = rfq.rfq_route(l, k)
+    return l, x, z, w, rfq.rfq_expert_sort(experts, E)
+
+
+CALLS = {
+    # The differentiable argument and the call on it and the others.
+    "route": (0, lambda t, l, x, z, w, plan, s: rfq.rfq_route(t, k, stream=s)[0]),
+    "route over all": (0, lambda t, l, x, z, w, plan, s: rfq.rfq_route(t, k, False, stream=s)[0]),
+    "gather": (1, lambda t, l, x, z, w, plan, s: rfq.rfq_expert_gather(t, plan, stream=s)),
+    "combine, z": (2, lambda t, l, x, z, w, plan, s: rfq.rfq_expert_combine(t, w, plan, stream=s)),
+    "combine, weights": (3, lambda t, l, x, z, w, plan, s: rfq.rfq_expert_combine(z, t, plan, stream=s)),
+    "combine without weights": (2, lambda t, l, x, z, w, plan, s: rfq.rfq_expert_combine(
+        t, None, plan, stream=s)),
+}
+
+
+@pytest.mark.parametrize("path", ["native", "python"])
+@pytest.mark.parametrize("name", CALLS)
+def test_a_tangent_is_refused(name, path):
+    at, f = CALLS[name]
+    args = inputs()
+    s = None if path == "native" else torch.cuda.current_stream()
+    t = args[at]
+    want = f(t, *args, s)
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(t, torch.ones_like(t))
+        for grad in (True, False):
+            with torch.set_grad_enabled(grad), pytest.raises(NotImplementedError, match="jvp"):
+                f(dual, *args, s)
+        # A tensor without a tangent is an ordinary one, also inside a level.
+        assert torch.equal(f(t, *args, s), want)
+        assert torch.equal(f(forward_ad.unpack_dual(dual).primal, *args, s), want)
+    assert torch.equal(f(dual, *args, s), want)         # the level has ended
+
+
+@pytest.mark.parametrize("path", ["native", "python"])
+def test_out_takes_no_tangent(path):
+    l, x, z, w, plan = inputs()
+    s = None if path == "native" else torch.cuda.current_stream()
+    with forward_ad.dual_level():
+        dx, dz, dw = (forward_ad.make_dual(t, torch.ones_like(t)) for t in (x, z, w))
+        with pytest.raises(ValueError, match="out takes no gradient"):
+            rfq.rfq_expert_gather(dx, plan, out=torch.empty_like(z), stream=s)
+        for a, b in ((dz, w), (z, dw), (dz, None)):
+            with pytest.raises(ValueError, match="out takes no gradient"):
+                rfq.rfq_expert_combine(a, b, plan, out=torch.empty_like(x), stream=s)
+        out = forward_ad.make_dual(torch.empty_like(x), x)
+        with pytest.raises(ValueError, match="out takes no gradient"):
+            rfq.rfq_expert_combine(z, w, plan, out=out, stream=s)
