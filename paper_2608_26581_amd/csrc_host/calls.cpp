@@ -89,6 +89,15 @@ int float_code(const at::Tensor &t) {
   return t.scalar_type() == at::kBFloat16 ? 1 : (t.scalar_type() == at::kFloat ? 0 : -1);
 }
 
+// Whether autograd would have to see a call on these (its Python path does that): one
+// requires a gradient, or has a tangent of the forward mode (torch has one level of it).
+template <class... T>
+bool wants_grad(const T *...t) {
+  return (at::GradMode::is_enabled() && ((t && t->requires_grad()) || ...)) ||
+         (c10::AutogradState::get_tls_state().get_fw_grad_mode() &&
+          ((t && t->_fw_grad(0).defined()) || ...));
+}
+
 // Releases the interpreter lock for its lifetime: an allocation may have to
 // wait for the driver and a launch for room in a full queue, and a host
 // callback that the queue waits for may need the lock.
@@ -555,7 +564,7 @@ PyObject *rope(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (inter < 0) return nullptr;
   if (!rope_spec(a[1], a[2], a[3], inter, x->size(0), dev, spec)) return none();
   const at::Tensor y = heads_out(a[5], *x, dev, hy);
-  if (!y.defined()) return none();
+  if (!y.defined() || wants_grad(x, &y)) return none();
   const int st = call(BACKWARD ? kv.rope_backward : kv.rope, &hx, float_code(*x), x->size(0),
                       x->size(1), x->size(2), &spec, &hy, stream_of(dev));
   return st ? failed(st) : result(a[5], y);
@@ -720,15 +729,6 @@ const float *float_data(const at::Tensor *t) {
 const at::Tensor *matrix(PyObject *o, int dev) {
   const at::Tensor *t = plain(o, dev);
   return t && float_code(*t) >= 0 ? t : nullptr;
-}
-
-// Whether autograd would have to see a call on these (its Python path does that): one
-// requires a gradient, or has a tangent of the forward mode (torch has one level of it).
-template <class... T>
-bool wants_grad(const T *...t) {
-  return (at::GradMode::is_enabled() && ((t && t->requires_grad()) || ...)) ||
-         (c10::AutogradState::get_tls_state().get_fw_grad_mode() &&
-          ((t && t->_fw_grad(0).defined()) || ...));
 }
 
 // A plan's tensors: rows [T k] and slots [T][k] (the offsets have only to be ints).

@@ -14,13 +14,12 @@ import threading
 from typing import NamedTuple
 
 import torch
-from torch.autograd.forward_ad import unpack_dual
 from torch.autograd.function import once_differentiable
 
 from . import rfq as _binding
 from .rfq import (
     _FLOAT, _OUT_CODE, _U8, _check, _dtype_code, _empty, _need, _need_pair, _ptr, _result, _stream,
-    _torch_stream, _written, _z_out, load,
+    _torch_stream, _wants_grad, _written, _z_out, load,
 )
 
 _I32 = (torch.int32,)
@@ -75,15 +74,6 @@ def _need_plan(plan, dev):
     _need_2d(slots, "slots", _I32, dev)
     _need(rows, "rows", _I32, (slots.numel(),), dev)
     return rows, slots
-
-
-def _wants_grad(*tensors):
-    """Whether autograd has to see a call on these: one requires a gradient, or has a tangent
-    of the forward mode, which the functions below do not have and torch then refuses."""
-    reverse = torch.is_grad_enabled()
-    return any(isinstance(t, torch.Tensor)
-               and (reverse and t.requires_grad or unpack_dual(t).tangent is not None)
-               for t in tensors)
 
 
 def _apply(function, stream, device, *args):

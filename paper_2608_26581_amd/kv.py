@@ -5,8 +5,9 @@ Each function carries the name of the C entry point it calls and checks its
 tensors as the other calls do.  q, k, v and outputs are [T][H][D] device tensors
 whose channels are contiguous; tokens and heads may be strided (slices of one
 joint projection).  A cache is a KvCache, or any four tensors of its layout.
-The rotation is differentiable; what goes through the 4-bit cache is not, and
-results of those calls carry no gradient.
+The rotation is differentiable in reverse mode (a tangent of the forward mode is an
+error); what goes through the 4-bit cache is not, and results of those calls carry no
+gradient.
 """
 import ctypes
 import threading
@@ -17,7 +18,7 @@ import torch
 from . import rfq as _binding
 from .rfq import (
     _FLOAT, _OUT_CODE, _U8, RFQ_BF16, RFQ_F32, Heads, KvCacheArgs, RopeSpec, _check, _dtype_code,
-    _empty, _need, _ptr, _result, _stream, _torch_stream, _written, load,
+    _empty, _need, _ptr, _result, _stream, _torch_stream, _wants_grad, _written, load,
 )
 
 _I32 = (torch.int32,)
@@ -229,8 +230,14 @@ class _Rope(torch.autograd.Function):
 
 
 def _rope_call(func, x, positions, cos_sin, axes, interleaved, out, stream):
-    if torch.is_grad_enabled() and isinstance(x, torch.Tensor) and (
-            x.requires_grad or getattr(out, "requires_grad", False)):
+    # (What requires a gradient is seen first; a tangent, the rare case, by the native call.)
+    grad = torch.is_grad_enabled() and isinstance(x, torch.Tensor) and (
+        x.requires_grad or getattr(out, "requires_grad", False))
+    if stream is None and not grad:
+        r = _native(func[4:], x, positions, cos_sin, axes, interleaved, out)
+        if r is not None:
+            return r if out is None else _written(out)
+    if grad or _wants_grad(x, out):
         if out is not None:
             raise ValueError("out takes no gradient: x and out must not require one")
         args = (x, positions, cos_sin, func, axes, interleaved)
@@ -241,10 +248,6 @@ def _rope_call(func, x, positions, cos_sin, axes, interleaved, out, stream):
             y = _Rope.apply(*args)
         y.record_stream(torch.cuda.current_stream(x.device))
         return y
-    if stream is None:
-        r = _native(func[4:], x, positions, cos_sin, axes, interleaved, out)
-        if r is not None:
-            return r if out is None else _written(out)
     _need_heads(x, "x", _FLOAT)
     dev = x.get_device()
     T, H, D = x.shape

@@ -16,6 +16,7 @@ import threading
 import warnings
 
 import torch
+from torch.autograd.forward_ad import unpack_dual
 
 _PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG_DIR, "librfq.so")
@@ -283,6 +284,15 @@ def _written(out):
     if not out.is_inference():
         torch.autograd.graph.increment_version(out)
     return out
+
+
+def _wants_grad(*tensors):
+    """Whether autograd has to see a call on these: one requires a gradient, or has a tangent
+    of the forward mode, which the differentiable calls do not have and torch then refuses."""
+    reverse = torch.is_grad_enabled()
+    return any(isinstance(t, torch.Tensor)
+               and (reverse and t.requires_grad or unpack_dual(t).tangent is not None)
+               for t in tensors)
 
 
 def _check(func, status):
