@@ -131,7 +131,8 @@ def rfq_route(logits, k, renormalize=True, stream=None):
     """The k largest of logits [T][E] (bf16 or fp32) per token, ties to the lower index ->
     (weights [T][k] fp32, experts [T][k] int32): softmax over the chosen logits, or with
     renormalize False over all.  -inf is not chosen: expert -1, weight 0.  weights are
-    differentiable in logits."""
+    differentiable in logits.  The two may be parts of one allocation (clone one that is to be
+    resized, or saved by itself)."""
     if stream is None:
         r = _native("route", logits, k, renormalize)
         if r is not None:
@@ -174,7 +175,8 @@ def rfq_expert_sort(experts, n_experts, first=0, workspace=None, stream=None):
     """The pairs of experts [T][k] sorted by expert, those of an expert in their order ->
     ExpertPlan.  Experts outside [first, first + n_experts) are dropped.  workspace: a
     contiguous uint8 tensor of rfq_expert_sort_workspace_bytes, or None: one from torch's
-    allocator.  The three may be parts of one allocation."""
+    allocator.  The three may be parts of one allocation (clone one that is to be
+    resized, or saved by itself)."""
     if stream is None:
         r = _native("expert_sort", experts, n_experts, first, workspace)
         if r is not None:
