@@ -122,7 +122,8 @@ __global__ __launch_bounds__(kThreads) void expert_gather_kernel(
   }
 }
 
-// One piece a lane; the rows of kBatch choices are loaded together.
+// One piece a lane; the rows of kBatch choices are loaded together.  8192 tokens of 8 choices: 2048
+// bf16 channels 57.3 us (5.3 TB/s), 512 12.5, 64 7.2; 2049, element by element, 182 (1.7).
 template <bool BF16, bool VEC>
 __global__ __launch_bounds__(kThreads) void expert_combine_kernel(
     const void *__restrict__ z, int64_t P, int pieces, const int32_t *__restrict__ slots,
@@ -165,7 +166,9 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
-// A workgroup a token; those past the tokens write the zeros of dz, 64 slots each.
+// A workgroup a token; those past the tokens write the zeros of dz, 64 slots each.  8192 tokens of 8
+// choices: 2048 bf16 channels 112 us (5.1 TB/s), 512 32.5 (4.4), 64 26.1, bound by the workgroups' own
+// latency; 2049, element by element, 258 (2.2).
 template <bool BF16, bool VEC, int kMost>
 __global__ __launch_bounds__(kThreads) void expert_combine_backward_kernel(
     const void *__restrict__ dout, const void *__restrict__ z, int64_t P, int pieces,

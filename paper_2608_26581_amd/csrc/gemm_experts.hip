@@ -6,8 +6,8 @@
 // prefix sum over the experts' (experts_device.h).
 //
 // Experts with few slots are bound by streaming their weights, those with many by the
-// matrix cores.  Two launches, by the mean number of slots (P / E; the lengths themselves are
-// on the device):
+// matrix cores.  Two launches, by P / E, the mean number of slots where every pair's expert is
+// held here (the lengths themselves are on the device; use_many()):
 //   both   128 x 128 tiles of the dense product (gemm_tile.h) for the experts with more than
 //          16 slots, and in the same launch tiles of 16 slots by 64 weight rows for the others;
 //   many   256 x 256 tiles of the dense product, or 128 x 256 at an expert's end.
@@ -49,6 +49,12 @@ constexpr uint32_t kNowhere = 0x80000000u;      // an offset past every buffer: 
 // 23 without them.  FAST (K a multiple of 128 and at most kFewK): those of 64 weight rows are
 // one run of memory, which the workgroup copies 16 bytes a lane, and those of q and r whole
 // dwords.
+//
+// Other K stage their scale bytes in pieces of kFewK columns, whole dwords where K is a
+// multiple of 128, else byte by byte.  Decode of 16 tokens that choose 68 of 128 experts of 1536
+// rows, us: K = 2048 26.2 (staged in pieces 32.4), 4096 44.3 (57.6); in pieces 4224 66.4, 5120 74.2,
+// 7168 97.3, byte by byte 2080 57.2.  With kFewK = 8192, whose scale bytes take twice the
+// registers, 2048 and 4096 take 26.6 and 44.6, and 4224, 5120 and 7168 49.6, 59.0 and 72.5.
 constexpr int kFrags = 4, kFewCols = 16 * kFrags;
 constexpr int kSteps = 2, kFewK = 4096, kFewBlocks = kFewK / 32;
 
@@ -369,6 +375,12 @@ hipError_t launch_many(const ExpertsGemm &g, const ExpertTiles &ex, hipStream_t 
 
 // 256 x 256 tiles from 96 slots an expert where 128 x 128 ones would number two a CU (8 experts
 // of 4096 x 4096: 256 slots each 51.6 us, both 62; 128 each, 384 tiles, 46 and 38).
+//
+// P counts the pairs that a share of a layer drops as well, so that a share's experts have fewer
+// slots than the rule takes them to have.  8 choices, K = 2048, us with these tiles and with
+// both: 64 of 128 experts of 1536 rows, 1024 tokens 49.4 and 45.7, 4096 tokens 88 and 96; 16 of 128
+// experts of 4096 rows, 256 tokens 17.1 and 18.0, 1024 tokens 33.5 and 26.2, 4096 tokens 63 and 66;
+// of 1536 rows, 1024 tokens 25.1 and 16.2, 4096 tokens 28.7 and 27.5.
 bool use_many(const ExpertsGemm &g) {
   return g.P >= 96 * (int64_t)g.E && (g.P / 128 + g.E / 2) * ((g.N + 127) / 128) >= 512;
 }

@@ -266,7 +266,13 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(
   }
 }
 
-// Calls go(shape) with the shape that holds E logits.
+// Calls go(shape) with the shape that holds E logits.  Where E is not a multiple of its R, logits
+// are loaded and gradients stored one by one (vector_rows()).  32768 tokens, 6 choices, softmax over
+// all, us, fp32 | bf16:             E =    80          144         176
+//   route                            8.3 | 6.7   10.8 | 8.9  12.2 | 10.0
+//   route in the next shape          8.8 | 6.8   10.7 | 8.3  12.9 |  9.8
+//   gradient                        10.4 | 7.6   20.6 | 13.0 28.7 | 17.0
+//   gradient in the next shape       8.4 | 8.0   10.8 | 10.6 15.2 | 12.0
 template <int L, int N>
 struct Shape {
   static constexpr int kLanes = L, R = N;
