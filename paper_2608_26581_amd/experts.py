@@ -14,6 +14,7 @@ import threading
 from typing import NamedTuple
 
 import torch
+from torch.autograd.forward_ad import unpack_dual
 from torch.autograd.function import once_differentiable
 
 from . import rfq as _binding
@@ -94,6 +95,14 @@ def _dense(t):
         memory_format=torch.contiguous_format)
 
 
+def _no_tangent(grad):
+    """Refuses a gradient with a tangent where the backward pass is differentiable in neither
+    mode (reverse mode is refused by once_differentiable)."""
+    if unpack_dual(grad).tangent is not None:
+        raise NotImplementedError("a backward pass of the calls around a layer of experts has no "
+                                  "jvp: its gradient must not have a tangent of the forward mode")
+
+
 # ---- the router
 
 class _Route(torch.autograd.Function):
@@ -108,6 +117,7 @@ class _Route(torch.autograd.Function):
     @staticmethod
     @once_differentiable
     def backward(ctx, dweights, _):
+        _no_tangent(dweights)
         logits, weights, experts = ctx.saved_tensors
         return rfq_route_backward(_dense(dweights), logits, weights, experts,
                                   ctx.renormalize), None, None
@@ -254,6 +264,7 @@ class _Combine(torch.autograd.Function):
     @staticmethod
     @once_differentiable
     def backward(ctx, dout):
+        _no_tangent(dout)
         z, weights, *plan = ctx.saved_tensors
         need_z, need_w = ctx.needs_input_grad[:2]
         dz, dw = _combine_backward(_dense(dout), z, weights, plan, need_z, need_w, None)

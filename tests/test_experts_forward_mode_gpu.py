@@ -66,3 +66,19 @@ def test_out_takes_no_tangent(path):
         out = forward_ad.make_dual(torch.empty_like(x), x)
         with pytest.raises(ValueError, match="out takes no gradient"):
             rfq.rfq_expert_combine(z, w, plan, out=out, stream=s)
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_a_tangent_of_the_gradient_is_refused(name):
+    """Forward mode over reverse: the gradient that comes to the backward pass has a tangent."""
+    at, f = CALLS[name]
+    args = inputs()
+    t = args[at].clone().requires_grad_()
+    y = f(t, *args, None)
+    want, = torch.autograd.grad(y.sum(), t, retain_graph=True)
+    with forward_ad.dual_level():
+        c = forward_ad.make_dual(torch.ones_like(y), torch.ones_like(y))
+        with pytest.raises(NotImplementedError, match="jvp"):
+            torch.autograd.grad((y * c).sum(), t, retain_graph=True)
+        got, = torch.autograd.grad(y.sum(), t, retain_graph=True)
+    assert torch.equal(got, want)

@@ -32,3 +32,14 @@ def test_a_tangent_is_refused(name, path):
         # A tensor without a tangent is an ordinary one, also inside a level.
         assert torch.equal(f(x, *rest, stream=s), want)
     assert torch.equal(f(dual, *rest, stream=s), want)  # the level has ended
+
+
+@pytest.mark.parametrize("name", ["rfq_rope", "rfq_rope_backward"])
+def test_a_tangent_of_the_gradient_is_refused(name):
+    """Forward mode over reverse: the gradient that comes to the backward pass has a tangent."""
+    x = torch.ones((5, 4, 64), device="cuda", requires_grad=True)
+    y = getattr(rfq, name)(x, torch.arange(5, device="cuda").int(), rfq.rope_table(9, 64))
+    with forward_ad.dual_level():
+        c = forward_ad.make_dual(torch.ones_like(y), torch.ones_like(y))
+        with pytest.raises(NotImplementedError, match="jvp"):
+            torch.autograd.grad((y * c).sum(), x)
